@@ -263,7 +263,7 @@ def _run_own(s):
     ints = {"offsets": route.offsets, "rows": route.rows}
     if s["kind"] == "product_8bit":
         xq, xs = gm.block_quantize(s["X"], 1)
-        return ints | {"P": gm.route_product_8bit(route, xq, xs, s["Wq"], s["Ws"], dtype=s["X"].dtype)}
+        return ints | {"P": gm.route_product_scaled(route, xq, xs, s["Wq"], s["Ws"], dtype=s["X"].dtype)}
     P = gm.route_product(route, s["X"], s["W"])
     if s["kind"] == "product":
         return ints | {"P": P}
