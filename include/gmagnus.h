@@ -35,7 +35,10 @@
 extern "C" {
 #endif
 
-typedef enum { GM_F32 = 0, GM_F64 = 1 } gm_dtype;
+typedef enum {
+  GM_F32 = 0, GM_F64 = 1,
+  GM_BF16 = 2, GM_F16 = 3, GM_E4M3 = 4 /* dense factors of the routed products only */
+} gm_dtype;
 
 enum {
   GM_OK = 0,
@@ -292,6 +295,80 @@ int gm_plan_get_row_products(const gm_plan* plan, int64_t* ip_out_device, void* 
  * Calls may overlap on the GPU (different streams, concurrent host threads) as long as they write different arrays. */
 #define GM_NOALLOC_MAX_NNZ_A 1048576
 int gm_row_products_noalloc(const gm_csr* A, const gm_csr* B, int64_t* ip_out_device, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Routed products: a sparse factor whose entries pick BLOCKS of the other factor.
+ *
+ * R is a CSR matrix with few columns and a few entries a row (which of E blocks of weights a row of X is
+ * multiplied by, and with what weight the results are added up: the layers of a mixture of experts).  With
+ * Gustavson's formula (Eq. 1) one level up, an entry of R picks a block where an entry of A picks a row of B:
+ *
+ *   P[p,:] = X[row(p),:] * W[col(p)]^T     for every entry of R        (gm_route_product)
+ *   Y[i,:] = sum of r * P[p,:] over the entries of row i of R          (gm_route_sum)
+ *
+ * The entries are used in the order of their columns ("places" p): column e has the places [offsets[e],
+ * offsets[e+1]), within a column the order of R is kept.  An entry whose column is outside [0, E) (-1, say) is
+ * routed nowhere: it has a place behind all others, its row of a result is zero, and it adds nothing.
+ * Unlike in the products above, columns need not ascend within a row.
+ *
+ * None of these calls waits for the device.  Work is enqueued on `cuda_stream`; scratch memory comes from the
+ * allocator hook and goes back to it, with that stream, before the call returns.  They can be captured into a
+ * CUDA graph once each kind has been called outside of a capture on the device; with a hook that
+ * serves captures (or the default pool).  Sums are kept in 32 bits, in an order that depends on the shapes
+ * and on R's structure only: the same call gives the same bits.
+ * ------------------------------------------------------------------------------------------- */
+
+/* A dense array in device memory: n_blocks matrices of n_rows x n_cols, element strides (not negative; 0 repeats).
+ * Results need contiguous rows (col_stride 1).  Inputs may have any strides; where base and strides are not
+ * multiples of 16 bytes, or no dimension is contiguous, the call first makes an aligned copy of them. */
+typedef struct gm_dense {
+  void* data;
+  int64_t n_blocks, n_rows, n_cols;
+  int64_t block_stride, row_stride, col_stride;
+  int32_t dtype; /* gm_dtype */
+  int32_t reserved;
+} gm_dense;
+
+typedef struct gm_route gm_route; /* opaque, owned by the library */
+
+#define GM_ROUTE_MAX_COLS 2048
+
+/* Puts the entries of R in the order of their columns (a stable counting sort).  R: f32 values, at most
+ * GM_ROUTE_MAX_COLS columns (else GM_ERR_CAPACITY).  The route borrows R's row_ptr and vals (read by gm_route_sum
+ * and its gradients, so values may change in between); col_idx is read by this call's kernel only.  A route can be used
+ * on other streams than the one it was made on when the caller orders them behind it, by any number of calls at a time. */
+int gm_route_plan(const gm_csr* R, void* cuda_stream, gm_route** route_out);
+/* Device arrays of the route, valid until it is destroyed: offsets (E + 1), and for every place its row of R and its entry;
+ * pos: the place of every entry. */
+int gm_route_arrays(const gm_route* route, const int64_t** offsets, const int32_t** rows, const int32_t** order, const int32_t** pos);
+/* GM_ERR_TIMEOUT when a kernel of an earlier call on this route gave up a wait (its results are then not valid), as
+ * every further call on it does; GM_OK otherwise.  Does not wait: synchronise first to know about all of them. */
+int gm_route_status(const gm_route* route);
+void gm_route_destroy(gm_route* route);
+
+/* P (nnz x N, by place) = row of X times W[column]^T.  W: E blocks of N x K, of X's type (bf16 or f16); P: f32, bf16 or
+ * f16.  X: n_rows x K, a row for each row of R, or with by_entry nnz x K, a row for each place (what an earlier product gave). */
+int gm_route_product(const gm_route* route, const gm_dense* X, int by_entry, const gm_dense* W, const gm_dense* P, void* cuda_stream);
+/* Gradients of gm_route_product.  dX: with by_entry dP[p,:] * W[column] for each place, else that summed over the entries of
+ * each row of R (in 32 bits, through nnz x K floats of scratch memory).  dW[e] = sum over the places p of column e of
+ * dP[p,:]^T * X[row(p),:]; blocks of columns without entries are zero.  Results: f32, bf16 or f16. */
+int gm_route_product_dx(const gm_route* route, const gm_dense* dP, const gm_dense* W, int by_entry, const gm_dense* dX, void* cuda_stream);
+int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dense* X, int by_entry, const gm_dense* dW, void* cuda_stream);
+
+/* Y (n_rows x N) = for each row of R the sum of its entries' rows of P, times the entries' values if `weighted`.  Rows without
+ * entries are zero.  Rows of P that are routed nowhere are not read. */
+int gm_route_sum(const gm_route* route, const gm_dense* P, int weighted, const gm_dense* Y, void* cuda_stream);
+/* Gradients of the weighted sum: dP[p,:] = r * dY[row(p),:] and dval[q] = <dY[row,:], P[place of q,:]>, by entry of R. */
+int gm_route_sum_grads(const gm_route* route, const gm_dense* dY, const gm_dense* P, const gm_dense* dP, float* dval, void* cuda_stream);
+
+/* X (bf16 or f16) in e4m3, with a scale for each block of block_rows (1 or 128) x 128 values: s = max(largest finite
+ * magnitude, 2^-100) / 448, q = x / s rounded to the nearest, ties to even, as the exact quotient would be.  Values that
+ * are not finite become NaN.  Q: X's shape, S: n_blocks x ceil(n_rows / block_rows) x ceil(n_cols / 128) f32, both contiguous. */
+int gm_block_quantize(const gm_dense* X, int block_rows, const gm_dense* Q, const gm_dense* S, void* cuda_stream);
+/* gm_route_product with e4m3 factors: P[p,n] = sum over blocks b of 128 k's of Xs[row,b] * Ws[col,n,b] * sum_k Xq * Wq.  Xs: a scale
+ * for each row and block; Ws: for each 128 rows (ceil(N / 128)) or each row (N) of a block of W.  P: f32, bf16 or f16. */
+int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_dense* Xs, int by_entry, const gm_dense* Wq, const gm_dense* Ws,
+                          const gm_dense* P, void* cuda_stream);
 
 /* Releases the arrays of a result produced by gm_spgemm_execute and zeroes the struct. */
 void gm_csr_free(gm_csr* C);

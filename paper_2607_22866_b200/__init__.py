@@ -16,6 +16,15 @@ from .binding import (  # noqa: F401
     spgemm_execute,
     spgemm,
     spgemm_host,
+    Route,
+    route_plan,
+    route_product,
+    route_product_dx,
+    route_product_dw,
+    route_sum,
+    route_sum_grads,
+    block_quantize,
+    route_product_scaled,
     load_library,
     EXPORTED_SYMBOLS,
 )

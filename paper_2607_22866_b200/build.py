@@ -8,7 +8,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
 _INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB_PATH = os.path.join(_HERE, "libgmagnus.so")
-_SOURCES = ["gm_api.cu", "gm_planner.cpp"]
+_SOURCES = ["gm_api.cu", "gm_route.cu", "gm_planner.cpp"]
 
 
 def _newest_source_mtime() -> float:
@@ -24,7 +24,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB_PATH + f".tmp{os.getpid()}"
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++20", "--threads", "0",
            "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared", "-I", _INCLUDE, "-I", _CSRC, "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]

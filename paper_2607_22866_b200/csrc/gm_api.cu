@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "gm_common.cuh"
+#include "gm_host.h"
 #include "gm_k1_analysis.cuh"
 #include "gm_k3_light.cuh"
 #include "gm_k3_rows.cuh"
@@ -35,23 +36,10 @@ namespace gm {
 // ------------------------------------------------------------------------------------------------
 static thread_local std::string g_last_error;
 
-static int fail(int code, const std::string& msg) {
+int fail(int code, const std::string& msg) {
   g_last_error = msg;
   return code;
 }
-
-#define GM_CUDA(expr)                                                                              \
-  do {                                                                                             \
-    cudaError_t e_ = (expr);                                                                       \
-    if (e_ != cudaSuccess)                                                                         \
-      return fail(GM_ERR_CUDA, std::string(#expr) + ": " + cudaGetErrorString(e_));               \
-  } while (0)
-
-#define GM_TRY(expr)                \
-  do {                              \
-    int rc_ = (expr);               \
-    if (rc_ != GM_OK) return rc_;   \
-  } while (0)
 
 struct Allocator {
   gm_alloc_fn alloc = nullptr;
@@ -79,7 +67,7 @@ static void* default_alloc(size_t bytes, cudaStream_t st) {
   return p;
 }
 
-static void* dev_alloc(size_t bytes, cudaStream_t st) {
+void* dev_alloc(size_t bytes, cudaStream_t st) {
   if (bytes == 0) bytes = 16;
   if (g_alloc.alloc) {
     void* p = g_alloc.alloc(bytes, st, g_alloc.user);
@@ -94,7 +82,7 @@ static void* dev_alloc(size_t bytes, cudaStream_t st) {
   }
   return default_alloc(bytes, st);
 }
-static void dev_free(void* p, cudaStream_t st) {
+void dev_free(void* p, cudaStream_t st) {
   if (!p) return;
   if (g_alloc.free) g_alloc.free(p, st, g_alloc.user);
   else cudaFreeAsync(p, st);
@@ -138,6 +126,14 @@ static int device_facts(DeviceFacts* out) {
     f.known = true;
   }
   *out = f;
+  return GM_OK;
+}
+
+int device_facts_basic(int* num_sms, int* smem_optin) {
+  DeviceFacts f;
+  GM_TRY(device_facts(&f));
+  *num_sms = f.num_sms;
+  *smem_optin = f.smem_optin;
   return GM_OK;
 }
 
@@ -213,6 +209,13 @@ static void give_slot(HostSlot* s) {
   std::lock_guard<std::mutex> lock(g_slot_mutex);
   g_free_slots.push_back(s);
 }
+
+int* take_error_word() {
+  HostSlot* s = take_slot();
+  return s ? s->err : nullptr;
+}
+void give_error_word(int* w) { give_slot(reinterpret_cast<HostSlot*>(w)); }  // (err is a slot's first member)
+static_assert(offsetof(HostSlot, err) == 0, "an error word is its slot");
 
 // ------------------------------------------------------------------------------------------------
 // plan

@@ -1,0 +1,159 @@
+// Sums over the entries of a row of R, and their gradients (R times dense rows, and the product sampled at R's entries).
+//
+//   k_route_sum        Y[i,:] = sum over the entries q of row i of r_q * P[pos[q],:]
+//   k_route_sum_grads  dP[pos[q],:] = r_q * dY[i,:],   dr_q = <dY[i,:], P[pos[q],:]>
+//
+// Both are bound by memory: P is read once (and dP written once), a row of Y or dY serves all entries of its row of R.  Sums are kept
+// in 32 bits, in the order of the row's entries, and rounded once.
+#pragma once
+#include "gm_r2_product.cuh"
+
+namespace gm {
+
+template <typename T> struct Vec8;  // eight consecutive values as floats
+template <> struct Vec8<float> {
+  static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+};
+template <> struct Vec8<__nv_bfloat16> {
+  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const u32 w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[8]) {
+    uint4 a;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<uint4*>(p) = a;
+  }
+};
+template <> struct Vec8<__half> {
+  static __device__ __forceinline__ void load(const __half* p, float (&v)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const __half2* h = reinterpret_cast<const __half2*>(&a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(h[i]);
+      v[2 * i] = f.x;
+      v[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ void store(__half* p, const float (&v)[8]) {
+    uint4 a;
+    __half2* h = reinterpret_cast<__half2*>(&a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<uint4*>(p) = a;
+  }
+};
+
+// kVec: rows are 16-byte aligned and a multiple of eight wide; a thread then has eight columns, else one.
+template <typename T, bool kVec>
+__device__ __forceinline__ void load_cols(const T* p, float (&v)[8]) {
+  if (kVec) Vec8<T>::load(p, v);
+  else v[0] = static_cast<float>(*p);
+}
+template <typename T, bool kVec>
+__device__ __forceinline__ void store_cols(T* p, const float (&v)[8]) {
+  if (kVec) Vec8<T>::store(p, v);
+  else *p = from_float<T>(v[0]);
+}
+
+struct SumArgs {
+  const i64* row_ptr;
+  const float* val;       // nullptr: every entry counts once
+  const i64* offsets;
+  const int32_t* rows;    // by place
+  const int32_t* order;   // by place
+  const int32_t* pos;     // by entry
+  int E;
+  i64 n_rows, entries;
+  int width;
+  const void* p;
+  i64 p_stride;
+  void* y;
+  i64 y_stride;
+};
+
+constexpr int kSumThreads = 128;
+
+template <typename TI, typename TO, bool kVec>
+__global__ void __launch_bounds__(kSumThreads) k_route_sum(const SumArgs a, int n_chunks) {
+  constexpr int kCols = kVec ? 8 : 1;
+  const i64 i = blockIdx.x / n_chunks;
+  const int c = (static_cast<int>(blockIdx.x % n_chunks) * kSumThreads + threadIdx.x) * kCols;
+  if (c >= a.width) return;
+  const i64 q0 = max(static_cast<i64>(0), a.row_ptr[i]), q1 = min(a.entries, a.row_ptr[i + 1]);
+  const int routed = static_cast<int>(a.offsets[a.E]);
+  const TI* p = static_cast<const TI*>(a.p) + c;
+  float acc[8] = {};
+  for (i64 q = q0; q < q1; q += 4) {  // four rows in flight
+    float v[4][8], r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      r[j] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[j][x] = 0.f;
+      if (q + j < q1) {
+        const int at = a.pos[q + j];
+        if (at < routed) {
+          r[j] = a.val ? a.val[q + j] : 1.f;
+          load_cols<TI, kVec>(p + at * a.p_stride, v[j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int x = 0; x < kCols; ++x) acc[x] = fmaf(r[j], v[j][x], acc[x]);
+  }
+  store_cols<TO, kVec>(static_cast<TO*>(a.y) + i * a.y_stride + c, acc);
+}
+
+// A warp per entry, in the order of the rows of R (so that a row's entries share its row of dY in cache).
+template <typename T, typename TD, bool kVec>
+__global__ void __launch_bounds__(256) k_route_sum_grads(const SumArgs a, TD* __restrict__ dp, i64 dp_stride, float* __restrict__ dval) {
+  constexpr int kCols = kVec ? 8 : 1;
+  const int lane = threadIdx.x & 31;
+  const i64 q = static_cast<i64>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  if (q >= a.entries) return;
+  const int at = a.pos[q];
+  TD* out = dp + at * dp_stride;
+  if (at >= a.offsets[a.E]) {  // routed nowhere
+    const float zero[8] = {};
+    for (int c = lane * kCols; c < a.width; c += 32 * kCols) store_cols<TD, kVec>(out + c, zero);
+    if (lane == 0) dval[q] = 0.f;
+    return;
+  }
+  const float r = a.val[q];
+  const T* dy = static_cast<const T*>(a.y) + a.rows[at] * a.y_stride;
+  const T* p = static_cast<const T*>(a.p) + at * a.p_stride;
+  float dot = 0.f;
+  for (int c = lane * kCols; c < a.width; c += 32 * kCols) {
+    float g[8], v[8];
+    load_cols<T, kVec>(dy + c, g);
+    load_cols<T, kVec>(p + c, v);
+#pragma unroll
+    for (int x = 0; x < kCols; ++x) {
+      dot = fmaf(g[x], v[x], dot);
+      g[x] *= r;
+    }
+    store_cols<TD, kVec>(out + c, g);
+  }
+  dot = warp_sum(dot);
+  if (lane == 0) dval[q] = dot;
+}
+
+}  // namespace gm

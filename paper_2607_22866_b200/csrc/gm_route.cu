@@ -1,0 +1,667 @@
+// C ABI of the routed products (see include/gmagnus.h): routes, products by a sparse factor whose entries pick blocks, their
+// gradients, sums over entries, 8-bit forms.  Nothing here waits for the device.
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <mutex>
+#include <new>
+
+#include "gm_host.h"
+#include "gm_r1_route.cuh"
+#include "gm_r2_product.cuh"
+#include "gm_r3_sum.cuh"
+#include "gm_r4_quantize.cuh"
+
+using gm::i64;
+
+struct gm_route {
+  i64 n_rows = 0, nnz = 0;
+  int E = 0;
+  const i64* row_ptr = nullptr;
+  const float* val = nullptr;
+  void* block = nullptr;  // offsets, rows, order, pos
+  i64* offsets = nullptr;
+  int32_t* rows = nullptr;
+  int32_t* order = nullptr;
+  int32_t* pos = nullptr;
+  int* err = nullptr;     // page-locked: the first problem of a kernel
+  cudaStream_t stream = nullptr;
+};
+
+namespace gm {
+
+static size_t elem_size(int dtype) {
+  switch (dtype) {
+    case GM_F32: return 4;
+    case GM_BF16: case GM_F16: return 2;
+    case GM_E4M3: return 1;
+    default: return 0;
+  }
+}
+static bool is_float_type(int dtype) { return dtype == GM_F32 || dtype == GM_BF16 || dtype == GM_F16; }
+
+static int check_dense(const gm_dense* M, const char* name) {
+  if (!M) return fail(GM_ERR_INVALID_ARG, std::string(name) + " is null");
+  if (M->n_blocks < 0 || M->n_rows < 0 || M->n_cols < 0 || M->n_blocks > INT32_MAX || M->n_rows > INT32_MAX - 65536 || M->n_cols > INT32_MAX - 65536)
+    return fail(GM_ERR_INVALID_ARG, std::string(name) + ": sizes out of range");
+  if (elem_size(M->dtype) == 0) return fail(GM_ERR_DTYPE, std::string(name) + ": unknown dtype");
+  if (M->block_stride < 0 || M->row_stride < 0 || M->col_stride < 0) return fail(GM_ERR_INVALID_ARG, std::string(name) + ": negative stride");
+  if (!M->data && M->n_blocks && M->n_rows && M->n_cols) return fail(GM_ERR_INVALID_ARG, std::string(name) + ": null data");
+  if (reinterpret_cast<uintptr_t>(M->data) % elem_size(M->dtype)) return fail(GM_ERR_INVALID_ARG, std::string(name) + ": data not aligned to its type");
+  return GM_OK;
+}
+// Results: rows contiguous, apart from each other.
+static int check_out(const gm_dense* M, const char* name) {
+  GM_TRY(check_dense(M, name));
+  if (M->n_cols > 1 && M->col_stride != 1) return fail(GM_ERR_INVALID_ARG, std::string(name) + ": rows of a result must be contiguous");
+  if ((M->n_rows > 1 && M->row_stride < M->n_cols) || (M->n_blocks > 1 && M->block_stride < (M->n_rows - 1) * M->row_stride + M->n_cols))
+    return fail(GM_ERR_INVALID_ARG, std::string(name) + ": rows of a result overlap");
+  return GM_OK;
+}
+static int check_shape(const gm_dense* M, const char* name, i64 blocks, i64 rows, i64 cols) {
+  if (M->n_blocks != blocks || M->n_rows != rows || M->n_cols != cols)
+    return fail(GM_ERR_DIM_MISMATCH, std::string(name) + ": " + std::to_string(M->n_blocks) + " x " + std::to_string(M->n_rows) + " x " + std::to_string(M->n_cols) +
+                                         " instead of " + std::to_string(blocks) + " x " + std::to_string(rows) + " x " + std::to_string(cols));
+  return GM_OK;
+}
+
+static PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
+static std::mutex g_encode_mutex;
+
+static int encoder(PFN_cuTensorMapEncodeTiled_v12000* out) {
+  std::lock_guard<std::mutex> lock(g_encode_mutex);
+  if (!g_encode) {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    GM_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found));
+    if (!f || found != cudaDriverEntryPointSuccess) return fail(GM_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+    g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+  }
+  *out = g_encode;
+  return GM_OK;
+}
+
+// rank 2 or 3; strides of the outer dimensions in bytes; 128-byte swizzle, what lies outside reads as zero.
+static int make_map(CUtensorMap* map, int dtype, int rank, const void* base, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+  PFN_cuTensorMapEncodeTiled_v12000 encode;
+  GM_TRY(encoder(&encode));
+  const uint32_t ones[3] = {1, 1, 1};
+  const CUtensorMapDataType type = dtype == GM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : dtype == GM_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  const CUresult rc = encode(map, type, rank, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (rc != CUDA_SUCCESS) return fail(GM_ERR_CUDA, "cuTensorMapEncodeTiled: error " + std::to_string(static_cast<int>(rc)));
+  return GM_OK;
+}
+
+// Memory of one call, given back in stream order when it ends.
+struct Scratch {
+  cudaStream_t st;
+  void* held[4] = {};
+  int n = 0;
+  explicit Scratch(cudaStream_t s) : st(s) {}
+  ~Scratch() { for (int i = 0; i < n; ++i) dev_free(held[i], st); }
+  void* get(size_t bytes) {
+    void* p = dev_alloc(bytes, st);
+    if (p) held[n++] = p;
+    return p;
+  }
+};
+
+// What a tensor map can be laid over: 16-byte aligned base and outer strides, none of them zero, the inner dimension contiguous.
+static bool map_fits(const gm_dense& M, bool rows_inner) {
+  const i64 es = static_cast<i64>(elem_size(M.dtype));
+  const i64 inner = rows_inner ? M.row_stride : M.col_stride, outer = rows_inner ? M.col_stride : M.row_stride;
+  const i64 n_inner = rows_inner ? M.n_rows : M.n_cols, n_outer = rows_inner ? M.n_cols : M.n_rows;
+  const auto ok = [&](i64 stride, i64 n) { return n <= 1 || (stride > 0 && stride * es % 16 == 0 && stride * es < (i64{1} << 40)); };
+  return reinterpret_cast<uintptr_t>(M.data) % 16 == 0 && (inner == 1 || n_inner <= 1) && ok(outer, n_outer) && ok(M.block_stride, M.n_blocks);
+}
+
+static int pack(const gm_dense& M, Scratch* mem, int num_sms, gm_dense* out) {
+  const i64 es = static_cast<i64>(elem_size(M.dtype)), per = 16 / es, padded = (M.n_cols + per - 1) / per * per;
+  const size_t bytes = static_cast<size_t>(M.n_blocks) * M.n_rows * padded * es;
+  void* p = mem->get(bytes);
+  if (!p) return fail(GM_ERR_OOM, "no room for an aligned copy of " + std::to_string(bytes) + " bytes");
+  const i64 total = M.n_blocks * M.n_rows * padded;
+  const unsigned grid = static_cast<unsigned>(std::min<i64>((total + 255) / 256, static_cast<i64>(num_sms) * 16));
+  if (es == 2)
+    k_route_pack<uint16_t><<<grid, 256, 0, mem->st>>>(static_cast<const uint16_t*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<uint16_t*>(p));
+  else if (es == 4)
+    k_route_pack<uint32_t><<<grid, 256, 0, mem->st>>>(static_cast<const uint32_t*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<uint32_t*>(p));
+  else
+    k_route_pack<uint8_t><<<grid, 256, 0, mem->st>>>(static_cast<const uint8_t*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<uint8_t*>(p));
+  GM_CUDA(cudaGetLastError());
+  *out = M;
+  out->data = p;
+  out->col_stride = 1;
+  out->row_stride = padded;
+  out->block_stride = M.n_rows * padded;
+  return GM_OK;
+}
+
+// Inputs of the kernels that read with ordinary loads: any block and row strides, rows contiguous.
+static int contiguous_rows(gm_dense* M, Scratch* mem) {
+  if (M->n_cols <= 1 || M->col_stride == 1 || M->n_rows == 0 || M->n_blocks == 0) return GM_OK;
+  int num_sms, smem_optin;
+  GM_TRY(device_facts_basic(&num_sms, &smem_optin));
+  return pack(gm_dense(*M), mem, num_sms, M);
+}
+
+// A map of rows: `box_rows` at a time (1: for loads of four rows by index).
+static int map_rows(CUtensorMap* map, gm_dense M, uint32_t box_rows, Scratch* mem, int num_sms) {
+  if (!map_fits(M, false)) GM_TRY(pack(gm_dense(M), mem, num_sms, &M));
+  const i64 es = static_cast<i64>(elem_size(M.dtype));
+  const uint64_t dims[2] = {static_cast<uint64_t>(M.n_cols), static_cast<uint64_t>(M.n_rows)};
+  const uint64_t strides[1] = {static_cast<uint64_t>(M.n_rows > 1 ? M.row_stride * es : (M.n_cols * es + 15) / 16 * 16)};
+  const uint32_t box[2] = {static_cast<uint32_t>(kRowBytes / es), box_rows};
+  return make_map(map, M.dtype, 2, M.data, dims, strides, box);
+}
+
+static int route_ready(const gm_route* r) {
+  if (!r) return fail(GM_ERR_INVALID_ARG, "route is null");
+  if (*static_cast<volatile int*>(r->err) != 0)
+    return fail(GM_ERR_TIMEOUT, "an earlier call on this route gave up waiting on the device: its results are not valid");
+  return GM_OK;
+}
+
+static int set_smem(const void* kernel, size_t bytes) {
+  GM_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+  return GM_OK;
+}
+
+constexpr size_t kT5Smem = static_cast<size_t>(kStages) * kStage + 1024 + sizeof(T5Block);
+static size_t product_smem(int E, bool bits8) {
+  return kT5Smem + static_cast<size_t>(E + 1) * 8 + (bits8 ? 16 + 2 * 4 * kTileN * 4 : 0);
+}
+static_assert(kT5Smem + (kRouteMaxCols + 1) * 8 + 16 + 2 * 4 * kTileN * 4 <= 232448, "fits a block's shared memory");
+
+// A result of no terms: rows of zeros.
+static int zero_out(const gm_dense& M, cudaStream_t st) {
+  const size_t es = elem_size(M.dtype);
+  if (M.n_cols == 0) return GM_OK;
+  for (i64 b = 0; b < M.n_blocks; ++b)
+    if (M.n_rows) GM_CUDA(cudaMemset2DAsync(static_cast<char*>(M.data) + static_cast<size_t>(b) * M.block_stride * es, static_cast<size_t>(M.n_rows > 1 ? M.row_stride : M.n_cols) * es, 0, M.n_cols * es, M.n_rows, st));
+  return GM_OK;
+}
+
+template <typename K>
+static int launch_t5(K kernel, i64 tiles, int num_sms, int threads, size_t smem, cudaStream_t st, const CUtensorMap& m0, const CUtensorMap& m1, const auto& args) {
+  GM_TRY(set_smem(reinterpret_cast<const void*>(kernel), smem));
+  kernel<<<static_cast<unsigned>(std::max<i64>(1, std::min<i64>(tiles, num_sms))), threads, smem, st>>>(m0, m1, args);
+  GM_CUDA(cudaGetLastError());
+  return GM_OK;
+}
+
+// out[p, m] = sum_k B[e(p)](m, k) X[x row of p, k];  w_transposed: B's rows are W's columns.
+static int product(const gm_route* r, const gm_dense& X, bool by_entry, const gm_dense& W, bool w_transposed, const gm_dense& out, cudaStream_t st) {
+  const i64 n_m = w_transposed ? W.n_cols : W.n_rows, n_k = w_transposed ? W.n_rows : W.n_cols;
+  if (r->nnz == 0 || n_m == 0) return GM_OK;
+  if (n_k == 0 || r->E == 0) return zero_out(out, st);
+  int num_sms, smem_optin;
+  GM_TRY(device_facts_basic(&num_sms, &smem_optin));
+  Scratch mem(st);
+  // the block of W as (rows m) x (sums over k): which of the two is contiguous decides the form in shared memory
+  gm_dense V = W;
+  if (w_transposed) {
+    std::swap(V.n_rows, V.n_cols);
+    std::swap(V.row_stride, V.col_stride);
+  }
+  bool m_inner = false;
+  if (!map_fits(V, false)) {
+    m_inner = map_fits(V, true);
+    if (!m_inner) {
+      gm_dense packed;
+      GM_TRY(pack(W, &mem, num_sms, &packed));
+      V = packed;
+      if (w_transposed) {
+        std::swap(V.n_rows, V.n_cols);
+        std::swap(V.row_stride, V.col_stride);
+        m_inner = true;
+      }
+    }
+  }
+  CUtensorMap map_w, map_x;
+  const i64 es = 2;
+  const i64 inner = m_inner ? V.n_rows : V.n_cols, outer = m_inner ? V.n_cols : V.n_rows, outer_stride = m_inner ? V.col_stride : V.row_stride;
+  const uint64_t row_bytes = static_cast<uint64_t>(outer > 1 ? outer_stride * es : (inner * es + 15) / 16 * 16);
+  const uint64_t dims[3] = {static_cast<uint64_t>(inner), static_cast<uint64_t>(outer), static_cast<uint64_t>(V.n_blocks)};
+  const uint64_t strides[2] = {row_bytes, V.n_blocks > 1 ? static_cast<uint64_t>(V.block_stride * es) : row_bytes * outer};
+  const uint32_t box[3] = {64, m_inner ? 64u : static_cast<uint32_t>(kTileM), 1};
+  GM_TRY(make_map(&map_w, V.dtype, 3, V.data, dims, strides, box));
+  GM_TRY(map_rows(&map_x, X, by_entry ? 32 : 1, &mem, num_sms));
+  ProductArgs a = {};
+  a.offsets = r->offsets;
+  a.rows = r->rows;
+  a.E = r->E;
+  a.n_m = static_cast<int>(n_m);
+  a.n_k = static_cast<int>(n_k);
+  a.x_rows = static_cast<int>(X.n_rows);
+  a.places = r->nnz;
+  a.out = out.data;
+  a.out_stride = out.row_stride;
+  a.type = X.dtype == GM_BF16 ? 1 : 0;
+  a.err = r->err;
+  const i64 tiles = ((r->nnz + kTileN - 1) / kTileN + std::min<i64>(r->E, r->nnz)) * ((n_m + kTileM - 1) / kTileM);
+  const size_t smem = product_smem(r->E, false);
+  const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, 192, smem, st, map_w, map_x, a); };
+  const auto typed = [&](auto* tag) {
+    using TO = std::remove_pointer_t<decltype(tag)>;
+    if (m_inner) return by_entry ? go(k_route_product<true, false, TO>) : go(k_route_product<true, true, TO>);
+    return by_entry ? go(k_route_product<false, false, TO>) : go(k_route_product<false, true, TO>);
+  };
+  switch (out.dtype) {
+    case GM_F32: return typed(static_cast<float*>(nullptr));
+    case GM_BF16: return typed(static_cast<__nv_bfloat16*>(nullptr));
+    default: return typed(static_cast<__half*>(nullptr));
+  }
+}
+
+static int sum_grid(i64 blocks, const char* what) {
+  return blocks > INT32_MAX ? fail(GM_ERR_INVALID_ARG, std::string(what) + ": too many rows and columns for one launch") : GM_OK;
+}
+
+static bool rows_aligned(const gm_dense& M) {
+  return reinterpret_cast<uintptr_t>(M.data) % 16 == 0 && M.n_cols % 8 == 0 && (M.n_rows <= 1 || M.row_stride * elem_size(M.dtype) % 16 == 0);
+}
+
+static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const gm_dense& Y, cudaStream_t st) {
+  if (Y.n_rows == 0 || Y.n_cols == 0) return GM_OK;
+  SumArgs a = {};
+  a.row_ptr = r->row_ptr;
+  a.val = weighted ? r->val : nullptr;
+  a.offsets = r->offsets;
+  a.rows = r->rows;
+  a.order = r->order;
+  a.pos = r->pos;
+  a.E = r->E;
+  a.n_rows = r->n_rows;
+  a.entries = r->nnz;
+  a.width = static_cast<int>(Y.n_cols);
+  a.p = P.data;
+  a.p_stride = P.row_stride;
+  a.y = Y.data;
+  a.y_stride = Y.row_stride;
+  const bool vec = rows_aligned(P) && rows_aligned(Y);
+  const i64 per = kSumThreads * (vec ? 8 : 1), chunks = (a.width + per - 1) / per;
+  GM_TRY(sum_grid(chunks * r->n_rows, "sum"));
+  const auto go = [&](auto kernel) {
+    kernel<<<static_cast<unsigned>(chunks * r->n_rows), kSumThreads, 0, st>>>(a, static_cast<int>(chunks));
+    GM_CUDA(cudaGetLastError());
+    return static_cast<int>(GM_OK);
+  };
+  const auto typed2 = [&](auto* ti, auto* to) {
+    using TI = std::remove_pointer_t<decltype(ti)>;
+    using TO = std::remove_pointer_t<decltype(to)>;
+    return vec ? go(k_route_sum<TI, TO, true>) : go(k_route_sum<TI, TO, false>);
+  };
+  const auto typed = [&](auto* ti) {
+    switch (Y.dtype) {
+      case GM_F32: return typed2(ti, static_cast<float*>(nullptr));
+      case GM_BF16: return typed2(ti, static_cast<__nv_bfloat16*>(nullptr));
+      default: return typed2(ti, static_cast<__half*>(nullptr));
+    }
+  };
+  switch (P.dtype) {
+    case GM_F32: return typed(static_cast<float*>(nullptr));
+    case GM_BF16: return typed(static_cast<__nv_bfloat16*>(nullptr));
+    default: return typed(static_cast<__half*>(nullptr));
+  }
+}
+
+static int guarded(const auto& body) {
+  try {
+    return body();
+  } catch (const std::bad_alloc&) {
+    return GM_ERR_OOM;
+  } catch (...) {
+    return GM_ERR_INTERNAL;
+  }
+}
+
+static int check_products(const gm_dense* X, const gm_dense* W, const gm_dense* out, const char* x_name, const char* out_name) {
+  if (X->dtype != GM_BF16 && X->dtype != GM_F16) return fail(GM_ERR_DTYPE, std::string(x_name) + ": bf16 or f16 expected");
+  if (W && W->dtype != X->dtype) return fail(GM_ERR_DTYPE, "the factors' types differ");
+  if (!is_float_type(out->dtype)) return fail(GM_ERR_DTYPE, std::string(out_name) + ": f32, bf16 or f16 expected");
+  return GM_OK;
+}
+
+}  // namespace gm
+
+using namespace gm;
+
+extern "C" {
+
+int gm_route_plan(const gm_csr* R, void* cuda_stream, gm_route** route_out) {
+  return guarded([&]() -> int {
+    if (!R || !route_out) return fail(GM_ERR_INVALID_ARG, "null argument");
+    *route_out = nullptr;
+    if (R->n_rows < 0 || R->n_cols < 0 || R->nnz < 0 || R->n_rows > INT32_MAX - 65536 || R->nnz > INT32_MAX - 65536)
+      return fail(GM_ERR_INVALID_ARG, "R: sizes out of range");
+    if (R->n_cols > kRouteMaxCols) return fail(GM_ERR_CAPACITY, "R: more than " + std::to_string(kRouteMaxCols) + " columns");
+    if (R->n_rows == 0 && R->nnz > 0) return fail(GM_ERR_BAD_CSR, "R: entries without rows");
+    if (!R->row_ptr || (R->nnz > 0 && (!R->col_idx || !R->vals))) return fail(GM_ERR_INVALID_ARG, "R: null array");
+    if (R->dtype != GM_F32) return fail(GM_ERR_DTYPE, "R: f32 values expected");
+    int num_sms, smem_optin;
+    GM_TRY(device_facts_basic(&num_sms, &smem_optin));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    gm_route* r = new (std::nothrow) gm_route;
+    if (!r) return fail(GM_ERR_OOM, "out of host memory");
+    const auto drop = [&](int rc) { gm_route_destroy(r); return rc; };
+    r->n_rows = R->n_rows;
+    r->nnz = R->nnz;
+    r->E = static_cast<int>(R->n_cols);
+    r->row_ptr = R->row_ptr;
+    r->val = static_cast<const float*>(R->vals);
+    r->stream = st;
+    r->err = take_error_word();
+    if (!r->err) return drop(fail(GM_ERR_OOM, "no page-locked memory"));
+    const size_t n_off = (static_cast<size_t>(r->E + 1) * 8 + 15) / 16 * 16, n_arr = (static_cast<size_t>(r->nnz) * 4 + 15) / 16 * 16;
+    r->block = dev_alloc(n_off + 3 * n_arr, st);
+    if (!r->block) return drop(fail(GM_ERR_OOM, "no room for the route"));
+    char* p = static_cast<char*>(r->block);
+    r->offsets = reinterpret_cast<i64*>(p);
+    r->rows = reinterpret_cast<int32_t*>(p + n_off);
+    r->order = reinterpret_cast<int32_t*>(p + n_off + n_arr);
+    r->pos = reinterpret_cast<int32_t*>(p + n_off + 2 * n_arr);
+    // one block up to 4096 entries (four per thread), then as many as give every thread that many
+    const int warps = route_warps(r->E);
+    unsigned blocks = 1;
+    while (blocks < kRouteBlocks && static_cast<i64>(blocks) * warps * 32 * 4 < r->nnz) blocks *= 2;
+    const size_t smem = route_smem(r->E, warps);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(warps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = blocks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int rc = set_smem(reinterpret_cast<const void*>(k_route_plan), smem);
+    if (rc != GM_OK) return drop(rc);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_route_plan, r->row_ptr, R->col_idx, static_cast<int>(r->n_rows), r->nnz, r->E,
+                                             r->offsets, r->rows, r->order, r->pos);
+    if (e != cudaSuccess) return drop(fail(GM_ERR_CUDA, std::string("k_route_plan: ") + cudaGetErrorString(e)));
+    *route_out = r;
+    return GM_OK;
+  });
+}
+
+int gm_route_arrays(const gm_route* route, const int64_t** offsets, const int32_t** rows, const int32_t** order, const int32_t** pos) {
+  if (!route || !offsets || !rows || !order || !pos) return fail(GM_ERR_INVALID_ARG, "null argument");
+  *offsets = route->offsets;
+  *rows = route->rows;
+  *order = route->order;
+  *pos = route->pos;
+  return GM_OK;
+}
+
+int gm_route_status(const gm_route* route) { return guarded([&]() -> int { return route_ready(route); }); }
+
+void gm_route_destroy(gm_route* route) {
+  if (!route) return;
+  if (route->block) dev_free(route->block, route->stream);
+  give_error_word(route->err);
+  delete route;
+}
+
+int gm_route_product(const gm_route* route, const gm_dense* X, int by_entry, const gm_dense* W, const gm_dense* P, void* cuda_stream) {
+  return guarded([&]() -> int {
+    GM_TRY(route_ready(route));
+    GM_TRY(check_dense(X, "X"));
+    GM_TRY(check_dense(W, "W"));
+    GM_TRY(check_out(P, "P"));
+    GM_TRY(check_products(X, W, P, "X", "P"));
+    GM_TRY(check_shape(X, "X", 1, by_entry ? route->nnz : route->n_rows, W->n_cols));
+    GM_TRY(check_shape(W, "W", route->E, W->n_rows, W->n_cols));
+    GM_TRY(check_shape(P, "P", 1, route->nnz, W->n_rows));
+    return product(route, *X, by_entry != 0, *W, false, *P, static_cast<cudaStream_t>(cuda_stream));
+  });
+}
+
+int gm_route_product_dx(const gm_route* route, const gm_dense* dP, const gm_dense* W, int by_entry, const gm_dense* dX, void* cuda_stream) {
+  return guarded([&]() -> int {
+    GM_TRY(route_ready(route));
+    GM_TRY(check_dense(dP, "dP"));
+    GM_TRY(check_dense(W, "W"));
+    GM_TRY(check_out(dX, "dX"));
+    GM_TRY(check_products(dP, W, dX, "dP", "dX"));
+    GM_TRY(check_shape(dP, "dP", 1, route->nnz, W->n_rows));
+    GM_TRY(check_shape(W, "W", route->E, W->n_rows, W->n_cols));
+    GM_TRY(check_shape(dX, "dX", 1, by_entry ? route->nnz : route->n_rows, W->n_cols));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (by_entry) return product(route, *dP, true, *W, true, *dX, st);
+    if (route->nnz == 0) return zero_out(*dX, st);
+    // the entries' terms in 32 bits, then one sum per row of R: each result is rounded once
+    Scratch mem(st);
+    gm_dense T = {};
+    T.n_blocks = 1;
+    T.n_rows = route->nnz;
+    T.n_cols = W->n_cols;
+    T.row_stride = (W->n_cols + 7) / 8 * 8;
+    T.col_stride = 1;
+    T.dtype = GM_F32;
+    T.data = mem.get(static_cast<size_t>(T.n_rows) * T.row_stride * 4);
+    if (!T.data) return fail(GM_ERR_OOM, "no room for the entries' terms");
+    GM_TRY(product(route, *dP, true, *W, true, T, st));
+    return sum_rows(route, T, false, *dX, st);
+  });
+}
+
+int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dense* X, int by_entry, const gm_dense* dW, void* cuda_stream) {
+  return guarded([&]() -> int {
+    GM_TRY(route_ready(route));
+    GM_TRY(check_dense(dP, "dP"));
+    GM_TRY(check_dense(X, "X"));
+    GM_TRY(check_out(dW, "dW"));
+    GM_TRY(check_products(dP, X, dW, "dP", "dW"));
+    GM_TRY(check_shape(dP, "dP", 1, route->nnz, dP->n_cols));
+    GM_TRY(check_shape(X, "X", 1, by_entry ? route->nnz : route->n_rows, X->n_cols));
+    GM_TRY(check_shape(dW, "dW", route->E, dP->n_cols, X->n_cols));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (dW->n_blocks == 0 || dW->n_rows == 0 || dW->n_cols == 0) return GM_OK;
+    if (route->nnz == 0) return zero_out(*dW, st);
+    int num_sms, smem_optin;
+    GM_TRY(device_facts_basic(&num_sms, &smem_optin));
+    Scratch mem(st);
+    CUtensorMap map_p, map_x;
+    GM_TRY(map_rows(&map_p, *dP, 1, &mem, num_sms));
+    GM_TRY(map_rows(&map_x, *X, 1, &mem, num_sms));
+    DwArgs a = {};
+    a.offsets = route->offsets;
+    a.rows = by_entry ? nullptr : route->rows;
+    a.E = route->E;
+    a.n_m = static_cast<int>(dP->n_cols);
+    a.n_j = static_cast<int>(X->n_cols);
+    a.x_rows = static_cast<int>(X->n_rows);
+    a.places = route->nnz;
+    a.out = dW->data;
+    a.out_block = dW->block_stride;
+    a.out_stride = dW->row_stride;
+    a.type = dP->dtype == GM_BF16 ? 1 : 0;
+    a.err = route->err;
+    const i64 tiles = static_cast<i64>(a.E) * ((a.n_m + kTileM - 1) / kTileM) * ((a.n_j + kTileN - 1) / kTileN);
+    const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, 192, kT5Smem, st, map_p, map_x, a); };
+    switch (dW->dtype) {
+      case GM_F32: return by_entry ? go(k_route_dw<false, float>) : go(k_route_dw<true, float>);
+      case GM_BF16: return by_entry ? go(k_route_dw<false, __nv_bfloat16>) : go(k_route_dw<true, __nv_bfloat16>);
+      default: return by_entry ? go(k_route_dw<false, __half>) : go(k_route_dw<true, __half>);
+    }
+  });
+}
+
+int gm_route_sum(const gm_route* route, const gm_dense* P, int weighted, const gm_dense* Y, void* cuda_stream) {
+  return guarded([&]() -> int {
+    GM_TRY(route_ready(route));
+    GM_TRY(check_dense(P, "P"));
+    GM_TRY(check_out(Y, "Y"));
+    if (!is_float_type(P->dtype) || !is_float_type(Y->dtype)) return fail(GM_ERR_DTYPE, "f32, bf16 or f16 expected");
+    GM_TRY(check_shape(P, "P", 1, route->nnz, P->n_cols));
+    GM_TRY(check_shape(Y, "Y", 1, route->n_rows, P->n_cols));
+    Scratch mem(static_cast<cudaStream_t>(cuda_stream));
+    gm_dense V = *P;
+    GM_TRY(contiguous_rows(&V, &mem));
+    return sum_rows(route, V, weighted != 0, *Y, mem.st);
+  });
+}
+
+int gm_route_sum_grads(const gm_route* route, const gm_dense* dY, const gm_dense* P, const gm_dense* dP, float* dval, void* cuda_stream) {
+  return guarded([&]() -> int {
+    GM_TRY(route_ready(route));
+    GM_TRY(check_dense(dY, "dY"));
+    GM_TRY(check_dense(P, "P"));
+    GM_TRY(check_out(dP, "dP"));
+    if (!is_float_type(dY->dtype) || P->dtype != dY->dtype || dP->dtype != dY->dtype) return fail(GM_ERR_DTYPE, "dY, P and dP of one type (f32, bf16 or f16) expected");
+    GM_TRY(check_shape(P, "P", 1, route->nnz, P->n_cols));
+    GM_TRY(check_shape(dY, "dY", 1, route->n_rows, P->n_cols));
+    GM_TRY(check_shape(dP, "dP", 1, route->nnz, P->n_cols));
+    if (route->nnz == 0) return GM_OK;
+    if (!dval) return fail(GM_ERR_INVALID_ARG, "dval is null");
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    Scratch mem(st);
+    gm_dense G = *dY, V = *P;
+    GM_TRY(contiguous_rows(&G, &mem));
+    GM_TRY(contiguous_rows(&V, &mem));
+    SumArgs a = {};
+    a.row_ptr = route->row_ptr;
+    a.val = route->val;
+    a.offsets = route->offsets;
+    a.rows = route->rows;
+    a.pos = route->pos;
+    a.E = route->E;
+    a.n_rows = route->n_rows;
+    a.entries = route->nnz;
+    a.width = static_cast<int>(P->n_cols);
+    a.p = V.data;
+    a.p_stride = V.row_stride;
+    a.y = G.data;
+    a.y_stride = G.row_stride;
+    const bool vec = rows_aligned(V) && rows_aligned(G) && rows_aligned(*dP);
+    const auto typed = [&](auto* tag) {
+      using T = std::remove_pointer_t<decltype(tag)>;
+      const auto kernel = vec ? k_route_sum_grads<T, T, true> : k_route_sum_grads<T, T, false>;
+      kernel<<<static_cast<unsigned>((route->nnz + 7) / 8), 256, 0, st>>>(a, static_cast<T*>(dP->data), dP->row_stride, dval);
+      GM_CUDA(cudaGetLastError());
+      return static_cast<int>(GM_OK);
+    };
+    switch (dY->dtype) {
+      case GM_F32: return typed(static_cast<float*>(nullptr));
+      case GM_BF16: return typed(static_cast<__nv_bfloat16*>(nullptr));
+      default: return typed(static_cast<__half*>(nullptr));
+    }
+  });
+}
+
+int gm_block_quantize(const gm_dense* X, int block_rows, const gm_dense* Q, const gm_dense* S, void* cuda_stream) {
+  return guarded([&]() -> int {
+    GM_TRY(check_dense(X, "X"));
+    GM_TRY(check_out(Q, "Q"));
+    GM_TRY(check_out(S, "S"));
+    if (block_rows != 1 && block_rows != 128) return fail(GM_ERR_INVALID_ARG, "block_rows: 1 or 128 expected");
+    if (X->dtype != GM_BF16 && X->dtype != GM_F16) return fail(GM_ERR_DTYPE, "X: bf16 or f16 expected");
+    if (Q->dtype != GM_E4M3 || S->dtype != GM_F32) return fail(GM_ERR_DTYPE, "Q: e4m3, S: f32 expected");
+    const i64 cg = (X->n_cols + 127) / 128, rg = (X->n_rows + block_rows - 1) / block_rows;
+    GM_TRY(check_shape(Q, "Q", X->n_blocks, X->n_rows, X->n_cols));
+    GM_TRY(check_shape(S, "S", X->n_blocks, rg, cg));
+    const auto dense = [](const gm_dense* M) {
+      return (M->n_rows <= 1 || M->row_stride == M->n_cols) && (M->n_blocks <= 1 || M->block_stride == M->n_rows * M->n_cols);
+    };
+    if (X->n_blocks == 0 || X->n_rows == 0 || X->n_cols == 0) return GM_OK;
+    if (!dense(Q) || !dense(S)) return fail(GM_ERR_INVALID_ARG, "Q and S must be contiguous");
+    QuantArgs a = {};
+    a.x = X->data;
+    a.x_block = X->block_stride;
+    a.x_row = X->row_stride;
+    a.x_col = X->col_stride;
+    a.n_blocks = X->n_blocks;
+    a.n_rows = X->n_rows;
+    a.n_cols = static_cast<int>(X->n_cols);
+    a.col_groups = static_cast<int>(cg);
+    a.q = static_cast<u32*>(Q->data);
+    a.s = static_cast<float*>(S->data);
+    const bool vec = X->col_stride == 1 && rows_aligned(*X) && (X->n_blocks <= 1 || X->block_stride % 8 == 0) && reinterpret_cast<uintptr_t>(Q->data) % 8 == 0;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const i64 units = X->n_blocks * rg * cg, blocks = block_rows == 1 ? (units + 15) / 16 : units;
+    GM_TRY(sum_grid(blocks, "quantize"));
+    const auto typed = [&](auto* tag) {
+      using T = std::remove_pointer_t<decltype(tag)>;
+      if (block_rows == 1) (vec ? k_quantize_rows<T, true> : k_quantize_rows<T, false>)<<<static_cast<unsigned>(blocks), 256, 0, st>>>(a);
+      else (vec ? k_quantize_tiles<T, true> : k_quantize_tiles<T, false>)<<<static_cast<unsigned>(blocks), 256, 0, st>>>(a, static_cast<int>(rg));
+      GM_CUDA(cudaGetLastError());
+      return static_cast<int>(GM_OK);
+    };
+    return X->dtype == GM_BF16 ? typed(static_cast<__nv_bfloat16*>(nullptr)) : typed(static_cast<__half*>(nullptr));
+  });
+}
+
+int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_dense* Xs, int by_entry, const gm_dense* Wq, const gm_dense* Ws,
+                          const gm_dense* P, void* cuda_stream) {
+  return guarded([&]() -> int {
+    GM_TRY(route_ready(route));
+    GM_TRY(check_dense(Xq, "Xq"));
+    GM_TRY(check_dense(Xs, "Xs"));
+    GM_TRY(check_dense(Wq, "Wq"));
+    GM_TRY(check_dense(Ws, "Ws"));
+    GM_TRY(check_out(P, "P"));
+    if (Xq->dtype != GM_E4M3 || Wq->dtype != GM_E4M3) return fail(GM_ERR_DTYPE, "Xq and Wq: e4m3 expected");
+    if (Xs->dtype != GM_F32 || Ws->dtype != GM_F32) return fail(GM_ERR_DTYPE, "Xs and Ws: f32 expected");
+    if (!is_float_type(P->dtype)) return fail(GM_ERR_DTYPE, "P: f32, bf16 or f16 expected");
+    const i64 cg = (Wq->n_cols + 127) / 128, x_rows = by_entry ? route->nnz : route->n_rows;
+    GM_TRY(check_shape(Xq, "Xq", 1, x_rows, Wq->n_cols));
+    GM_TRY(check_shape(Xs, "Xs", 1, x_rows, cg));
+    GM_TRY(check_shape(Wq, "Wq", route->E, Wq->n_rows, Wq->n_cols));
+    const bool row_scales = Ws->n_rows == Wq->n_rows && Wq->n_rows > 1;  // (of one row the two forms are the same)
+    GM_TRY(check_shape(Ws, "Ws", route->E, row_scales ? Wq->n_rows : (Wq->n_rows + 127) / 128, cg));
+    GM_TRY(check_shape(P, "P", 1, route->nnz, Wq->n_rows));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (route->nnz == 0 || Wq->n_rows == 0) return GM_OK;
+    if (Wq->n_cols == 0 || route->E == 0) return zero_out(*P, st);
+    int num_sms, smem_optin;
+    GM_TRY(device_facts_basic(&num_sms, &smem_optin));
+    Scratch mem(st);
+    gm_dense V = *Wq, xs = *Xs, ws = *Ws;
+    GM_TRY(contiguous_rows(&xs, &mem));
+    GM_TRY(contiguous_rows(&ws, &mem));
+    if (!map_fits(V, false)) GM_TRY(pack(*Wq, &mem, num_sms, &V));
+    CUtensorMap map_w, map_x;
+    const uint64_t row_bytes = static_cast<uint64_t>(V.n_rows > 1 ? V.row_stride : (V.n_cols + 15) / 16 * 16);
+    const uint64_t dims[3] = {static_cast<uint64_t>(V.n_cols), static_cast<uint64_t>(V.n_rows), static_cast<uint64_t>(V.n_blocks)};
+    const uint64_t strides[2] = {row_bytes, V.n_blocks > 1 ? static_cast<uint64_t>(V.block_stride) : row_bytes * V.n_rows};
+    const uint32_t box[3] = {kRowBytes, kTileM, 1};
+    GM_TRY(make_map(&map_w, GM_E4M3, 3, V.data, dims, strides, box));
+    GM_TRY(map_rows(&map_x, *Xq, by_entry ? 32 : 1, &mem, num_sms));
+    ProductArgs a = {};
+    a.offsets = route->offsets;
+    a.rows = route->rows;
+    a.E = route->E;
+    a.n_m = static_cast<int>(Wq->n_rows);
+    a.n_k = static_cast<int>(Wq->n_cols);
+    a.x_rows = static_cast<int>(Xq->n_rows);
+    a.places = route->nnz;
+    a.out = P->data;
+    a.out_stride = P->row_stride;
+    a.type = 0;
+    a.xs = static_cast<const float*>(xs.data);
+    a.xs_stride = xs.row_stride;
+    a.ws = static_cast<const float*>(ws.data);
+    a.ws_block = ws.block_stride;
+    a.ws_row = ws.row_stride;
+    a.err = route->err;
+    const i64 tiles = ((route->nnz + kTileN - 1) / kTileN + std::min<i64>(route->E, route->nnz)) * ((a.n_m + kTileM - 1) / kTileM);
+    const size_t smem = product_smem(route->E, true);
+    const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, 320, smem, st, map_w, map_x, a); };
+    const auto typed = [&](auto* tag) {
+      using TO = std::remove_pointer_t<decltype(tag)>;
+      if (row_scales) return by_entry ? go(k_route_product8<false, true, TO>) : go(k_route_product8<true, true, TO>);
+      return by_entry ? go(k_route_product8<false, false, TO>) : go(k_route_product8<true, false, TO>);
+    };
+    switch (P->dtype) {
+      case GM_F32: return typed(static_cast<float*>(nullptr));
+      case GM_BF16: return typed(static_cast<__nv_bfloat16*>(nullptr));
+      default: return typed(static_cast<__half*>(nullptr));
+    }
+  });
+}
+
+}  // extern "C"

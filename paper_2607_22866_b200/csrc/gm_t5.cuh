@@ -1,0 +1,108 @@
+// Thin wrappers of the sm_100a instructions that the routed products use: tensor-map copies into shared memory, matrix
+// instructions on tensor memory, and the waits between them (every one bounded).
+#pragma once
+#include <cuda.h>
+
+#include "gm_common.cuh"
+
+namespace gm {
+
+// Polls of a barrier before a wait gives up: a failed try_wait has itself waited for a while, so this is far above any
+// wait that ends (the longest is for one tile's products, under 2 ms).
+constexpr int kT5SpinLimit = 1 << 22;
+
+// Without back-off: these barriers hand over within a microsecond.
+__device__ __forceinline__ bool t5_wait(u64* bar, u32 parity) {
+  for (int i = 0; i < kT5SpinLimit; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  return false;
+}
+__device__ __forceinline__ void mbar_arrive(u64* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(u32 dst, const CUtensorMap* map, int x, int y, u64* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(u32 dst, const CUtensorMap* map, int x, int y, int z, u64* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+               : "memory");
+}
+// four rows of the map (its box is one row high) into four consecutive 128-byte rows
+__device__ __forceinline__ void tma_gather4(u32 dst, const CUtensorMap* map, int x, int4 r, u64* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "r"(smem_u32(bar))
+      : "memory");
+}
+
+// Tensor memory: a whole warp allocates and frees.
+__device__ __forceinline__ void tmem_alloc(u32* where, u32 columns) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(u32 addr, u32 columns) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void t5_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void t5_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// arrives on `bar` when the matrix instructions issued so far by this thread are done
+__device__ __forceinline__ void t5_commit(u64* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// 32 columns of this warp's 32 lanes: v[j] = lane's value in column addr + j.  t5_wait_ld() before the values are used.
+__device__ __forceinline__ void t5_ld32(u32 (&v)[32], u32 addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]),
+        "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]),
+        "=r"(v[30]), "=r"(v[31])
+      : "r"(addr));
+}
+__device__ __forceinline__ void t5_ld16(u32 (&v)[16], u32 addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void t5_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// Descriptor of an operand in shared memory, 128-byte swizzle, the reduction along the 128-byte rows ("K-major"):
+// groups of 8 rows lie 1024 bytes apart.
+__device__ __forceinline__ u64 t5_desc_k(u32 addr) {
+  return (static_cast<u64>(2) << 61) | (static_cast<u64>(1) << 46) | (static_cast<u64>(1024 >> 4) << 32) | (static_cast<u64>(1) << 16) | ((addr & 0x3ffff) >> 4);
+}
+// The same with the reduction across the rows ("MN-major"): 64 values of the operand's own dimension in a 128-byte row, 8 steps
+// of the reduction in 1024 bytes, the next 64 values `block` bytes on.
+__device__ __forceinline__ u64 t5_desc_mn(u32 addr, u32 block) {
+  return (static_cast<u64>(2) << 61) | (static_cast<u64>(1) << 46) | (static_cast<u64>(1024 >> 4) << 32) | (static_cast<u64>(block >> 4) << 16) | ((addr & 0x3ffff) >> 4);
+}
+// Instruction descriptor: 32-bit sums; type 0 / 1 of both operands (f16 / bf16, or e4m3 / e5m2), MN-major flags, sizes.
+__device__ __forceinline__ u32 t5_idesc(u32 type, bool a_mn, bool b_mn, u32 m, u32 n) {
+  return (1u << 4) | (type << 7) | (type << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+__device__ __forceinline__ void t5_mma_f16(u32 d, u64 a, u64 b, u32 idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
+      : "memory");
+}
+__device__ __forceinline__ void t5_mma_f8(u32 d, u64 a, u64 b, u32 idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
+      : "memory");
+}
+
+}  // namespace gm
