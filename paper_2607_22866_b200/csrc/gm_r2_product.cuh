@@ -1,8 +1,17 @@
 // Routed products on the 5th-generation tensor cores (tcgen05, sums in tensor memory).
 //
-//   k_route_product    out[p, m] = sum_k  W[e(p)][m, k] * X[row(p), k]      p: place in the order of the columns of R
-//   k_route_product8   the same with e4m3 operands and a scale per 128 values of k
-//   k_route_dw         dW[e][m, j] = sum over the places p of column e of dP[p, m] * X[row(p), j]
+//   k_route_product         out[p, m] = sum_k  W[e(p)][m, k] * X[row(p), k]      p: place in the order of the columns of R
+//   k_route_product_scaled  the same with e4m3 operands and a scale per 128 values of k
+//   k_route_dw              dW[e][m, j] = sum over the places p of column e of dP[p, m] * X[row(p), j]
+//
+// All three work on tiles of 256 x 256 sums, a pair of blocks (of neighbouring SMs) each: either block brings in half of both
+// operands and keeps half of the sums, 256 columns by 128 lanes of its tensor memory.  A single block per 128 x 256 tile moves 1.5
+// times the bytes through shared memory per product, which then bounds it (1.03 against 1.3 PFLOP/s at 32768 x 2048 x 2048).
+// The places are the instruction's N: a column's places are cut into equal parts, and a part of 33 places costs matrix time for 64.
+// The sums have two buffers, so that the results of one tile are taken out while the next one is summed up.
+//
+// Rows of X are fetched by index with 16-byte asynchronous copies of four warps.  (Tensor-map loads of four rows by index took
+// about 50 cycles each however many warps issued them, four times what the matrix instructions take for those rows.)
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -11,19 +20,22 @@
 
 namespace gm {
 
-constexpr int kTileM = 128;        // rows of a block of W (or of dW) per tile: the lanes of tensor memory
-constexpr int kTileN = 256;        // places (or columns of dW) per tile: columns of tensor memory, twice
+constexpr int kTileM = 256;        // rows of a block of W (or of dW) per tile, half of them per block of threads
+constexpr int kTileN = 256;        // places (or columns of dW) per tile
 constexpr int kRowBytes = 128;     // of one operand row in a stage: 64 values of 16 bits, 128 of 8
-constexpr int kStages = 4;
-constexpr int kStageA = kTileM * kRowBytes, kStageB = kTileN * kRowBytes, kStage = kStageA + kStageB;
+constexpr int kStages = 6;
+constexpr int kHalf = 128 * kRowBytes;  // one block's share of an operand in a stage
+constexpr int kStage = 2 * kHalf;
+constexpr int kCopyThreads = 128;  // that fetch rows by index
 constexpr u32 kTmemColumns = 512;
 
 struct ProductArgs {
   const i64* offsets;
   const int32_t* rows;
   int E, n_m, n_k;      // columns of R, rows of a block of W, length of the sums
-  int x_rows;           // rows of X: the index that reads as zeros
   i64 places;           // entries of R
+  const char* x;        // rows by index: base, bytes from row to row
+  i64 x_stride;
   void* out;
   i64 out_stride;
   u32 type;             // of the operands in the instruction descriptor
@@ -36,12 +48,15 @@ struct ProductArgs {
 
 struct DwArgs {
   const i64* offsets;
-  const int32_t* rows;  // nullptr: X has a row per place
+  const int32_t* rows;
   int E, n_m, n_j;
-  int x_rows;
-  i64 places;
+  const char* dp;
+  i64 dp_stride;
+  const char* x;
+  i64 x_stride;
   void* out;
   i64 out_block, out_stride;
+  int out_align;        // bytes that every 32nd value's address is a multiple of
   u32 type;
   int* err;
 };
@@ -53,16 +68,17 @@ template <> __device__ __forceinline__ __half from_float<__half>(float v) { retu
 
 // The barriers and the place in tensor memory of a block, behind its stages.
 struct T5Block {
-  u64 full[kStages], empty[kStages];
+  u64 full[kStages], empty[kStages], copied[kStages];
   u64 sums_full[2], sums_empty[2], drain;
   u32 tmem;
   u32 scan_tmp[34];
 };
 
-// Places of each column, cut into parts of at most kTileN places that differ by less than 16 in size.
+// Places of each column, cut into parts of at most kTileN places that differ by less than 32 in size.
 struct Part { int e, first, n; };
+__device__ __forceinline__ int round32(int n) { return (n + 31) & ~31; }
 __device__ __forceinline__ int part_count(int places) { return (places + kTileN - 1) / kTileN; }
-__device__ __forceinline__ int part_size(int places, int parts) { return ((places + parts - 1) / parts + 15) & ~15; }
+__device__ __forceinline__ int part_size(int places, int parts) { return round32((places + parts - 1) / parts); }
 
 // off[e]: first place of column e; part[e]: parts of the columns before it.  All threads of the block.
 __device__ __forceinline__ void list_parts(const i64* __restrict__ offsets, int E, int* off, int* part, u32* scan_tmp) {
@@ -93,14 +109,13 @@ __device__ __forceinline__ Part part_at(const int* off, const int* part, int E, 
   return t;
 }
 
-__device__ __forceinline__ char* t5_align(char* p) {
-  return p + ((1024 - (smem_u32(p) & 1023)) & 1023);
-}
+__device__ __forceinline__ char* t5_align(char* p) { return p + ((1024 - (smem_u32(p) & 1023)) & 1023); }
 
-__device__ __forceinline__ void t5_begin(T5Block* b, int epilogue_warps) {
+// full_arrivals: on the leader's barrier of a stage, by both blocks;  result_warps: of one block.
+__device__ __forceinline__ void t5_begin(T5Block* b, int full_arrivals, int result_warps) {
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&b->sums_full[i], 1); mbar_init(&b->sums_empty[i], epilogue_warps); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&b->full[i], full_arrivals); mbar_init(&b->empty[i], 1); mbar_init(&b->copied[i], kCopyThreads); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&b->sums_full[i], 1); mbar_init(&b->sums_empty[i], 2 * result_warps); }
     mbar_init(&b->drain, 1);
     mbar_fence_init();
   }
@@ -108,12 +123,130 @@ __device__ __forceinline__ void t5_begin(T5Block* b, int epilogue_warps) {
   if (threadIdx.x < 32) tmem_alloc(&b->tmem, kTmemColumns);
   t5_fence_before();
   __syncthreads();
+  cluster_sync_all();
   t5_fence_after();
 }
-
-// A role that gave up waiting says so; copies in flight are waited for (with a limit) before the block leaves.
+// Both blocks leave together: neither's memory is gone while the other's instructions read it or arrive in it.
+__device__ __forceinline__ void t5_end(u32 tmem) {
+  t5_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  t5_fence_after();
+  if (threadIdx.x < 32) tmem_free(tmem, kTmemColumns);
+}
+// After a wait that gave up: the copies in flight are waited for (with a limit) before the blocks leave.
 __device__ __forceinline__ void t5_drain_copies(T5Block* b, u32 issued) {
   for (u32 i = issued > kStages ? issued - kStages : 0; i < issued; ++i) t5_wait(&b->full[i % kStages], (i / kStages) & 1);
+}
+__device__ __forceinline__ void t5_drain_matrix(T5Block* b) {
+  t5_commit(&b->drain);
+  t5_wait(&b->drain, 0);
+}
+
+// Rows by index: the copying threads go as far ahead as there are stages.  Their copies arrive on the stage's own barrier of the block;
+// one thread that has no copies under way itself makes them visible to the matrix instructions and tells the leader.  (A copying
+// thread's own fence waits for all its copies, the next stages' too: 43 us instead of 25 for a product of one row.)
+struct CopyQueue {
+  T5Block* b;
+  u32 issued = 0;
+  __device__ __forceinline__ explicit CopyQueue(T5Block* block) : b(block) {}
+  __device__ __forceinline__ bool slot_free() {
+    return __all_sync(0xffffffffu, t5_wait(&b->empty[issued % kStages], ((issued / kStages) & 1) ^ 1));
+  }
+  __device__ __forceinline__ void done() {  // the stage's copies are all issued
+    copy_arrive(&b->copied[issued % kStages]);
+    ++issued;
+  }
+};
+__device__ __forceinline__ bool hand_over(T5Block* b, u32 stage) {
+  if (!t5_wait(&b->copied[stage % kStages], (stage / kStages) & 1)) return false;
+  fence_to_matrix();
+  mbar_arrive_at(leader_bar(&b->full[stage % kStages]));
+  return true;
+}
+
+// The rows of X of one block's half of the places, for every tile and stage: eight lanes have a row of a stage.
+template <int kValueBytes>
+__device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u32 stage0, const int* off, const int* part, i64 n_tiles, int n_mt,
+                                            int thread) {
+  CopyQueue queue(b);
+  const int n_kb = (a.n_k * kValueBytes + kRowBytes - 1) / kRowBytes, c = thread & 7, r0 = thread >> 3;
+  const u32 at = kHalf + r0 * kRowBytes + ((c ^ (r0 & 7)) << 4);  // (rows r0 + 16 i: the same swizzle)
+  const i64 width = static_cast<i64>(a.n_k) * kValueBytes;
+  const u32 rank = cluster_rank();
+  bool ok = true;
+  for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+    const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+    const int half = round32(t.n) / 2;
+    const char* src[8];
+    u32 there = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + 16 * i, p = rank * half + r;
+      src[i] = a.x;
+      if (r < half && p < t.n) {
+        src[i] += a.rows[t.first + p] * a.x_stride;
+        there |= 1u << i;
+      }
+    }
+    for (int kb = 0; kb < n_kb; ++kb) {
+      ok = queue.slot_free();
+      if (!ok) break;
+      const u32 dst = stage0 + queue.issued % kStages * kStage + at;
+      const i64 x = static_cast<i64>(kb) * kRowBytes + c * 16;
+      const u32 bytes = static_cast<u32>(max(static_cast<i64>(0), min(static_cast<i64>(16), width - x)));
+      const i64 from = bytes ? x : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + 16 * i < half) copy16(dst + i * 16 * kRowBytes, src[i] + from, there >> i & 1 ? bytes : 0);
+      queue.done();
+    }
+  }
+  copy_wait_all();
+  if (!ok && (thread & 31) == 0) dev_set_error(a.err, kDevTimeout);
+}
+
+__device__ __forceinline__ void hand_over_rows(const ProductArgs& a, T5Block* b, i64 n_tiles, int n_kb) {
+  const i64 pairs = gridDim.x >> 1, mine = (n_tiles - (blockIdx.x >> 1) + pairs - 1) / pairs * n_kb;
+  bool ok = true;
+  for (i64 it = 0; ok && it < mine; ++it) ok = hand_over(b, static_cast<u32>(it));
+  if (!ok) dev_set_error(a.err, kDevTimeout);
+}
+
+// Tiles of W (and of X with a row per place) by tensor map.  One warp; lane 0 has W, lane i 32 rows of X.
+template <int kValueBytes, bool kAmn, bool kGather>
+__device__ __forceinline__ void copy_tiles(const ProductArgs& a, const CUtensorMap* map_w, const CUtensorMap* map_x, T5Block* b, u32 stage0,
+                                           const int* off, const int* part, i64 n_tiles, int n_mt) {
+  constexpr int kStep = kRowBytes / kValueBytes;
+  const int lane = threadIdx.x & 31, n_kb = (a.n_k + kStep - 1) / kStep;
+  const u32 rank = cluster_rank();
+  u32 it = 0;
+  bool ok = true;
+  for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+    const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+    const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128, half = round32(t.n) / 2;
+    const u32 bytes = 2 * (kHalf + (kGather ? 0 : round32(half) * kRowBytes));
+    for (int kb = 0; kb < n_kb; ++kb, ++it) {
+      const u32 s = it % kStages, sa = stage0 + s * kStage;
+      ok = __all_sync(0xffffffffu, t5_wait(&b->empty[s], ((it / kStages) & 1) ^ 1));
+      if (!ok) break;
+      const u32 bar = leader_bar(&b->full[s]);
+      if (lane == 0) {
+        if (rank == 0) mbar_arrive_expect_tx(&b->full[s], bytes);
+        if (kAmn) {
+          tma_load_3d(sa, map_w, m0, kb * kStep, t.e, bar);
+          tma_load_3d(sa + kHalf / 2, map_w, m0 + 64, kb * kStep, t.e, bar);
+        } else {
+          tma_load_3d(sa, map_w, kb * kStep, m0, t.e, bar);
+        }
+      }
+      if (!kGather && lane * 32 < half) tma_load_2d(sa + kHalf + lane * 32 * kRowBytes, map_x, kb * kStep, t.first + rank * half + lane * 32, bar);
+    }
+  }
+  if (!ok) {
+    if (lane == 0) dev_set_error(a.err, kDevTimeout);
+    if (rank == 0) t5_drain_copies(b, it);
+  }
 }
 
 // Rows of the result behind the last routed place are zero.
@@ -133,88 +266,79 @@ __device__ __forceinline__ void store_places(TO* __restrict__ out, i64 stride, i
   }
 }
 
+// 32 consecutive values of a row, of which n are stored; `align`: bytes that every such address is a multiple of (32, 16, less).
+template <typename TO>
+__device__ __forceinline__ void store_run(TO* __restrict__ out, int n, int align, const u32 (&v)[32]) {
+  if (align >= 16 && n >= 32) {
+    constexpr int kWords = 32 * sizeof(TO) / 4;
+    u32 w[kWords];
+    if constexpr (sizeof(TO) == 4) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) w[j] = v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const TO lo = from_float<TO>(__uint_as_float(v[2 * j])), hi = from_float<TO>(__uint_as_float(v[2 * j + 1]));
+        w[j] = static_cast<u32>(*reinterpret_cast<const uint16_t*>(&lo)) | (static_cast<u32>(*reinterpret_cast<const uint16_t*>(&hi)) << 16);
+      }
+    }
+    if (align >= 32) {  // whole sectors of 32 bytes
+#pragma unroll
+      for (int j = 0; j < kWords; j += 8)
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(reinterpret_cast<u32*>(out) + j), "r"(w[j]), "r"(w[j + 1]), "r"(w[j + 2]),
+                     "r"(w[j + 3]), "r"(w[j + 4]), "r"(w[j + 5]), "r"(w[j + 6]), "r"(w[j + 7])
+                     : "memory");
+    } else {
+#pragma unroll
+      for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(reinterpret_cast<u32*>(out) + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j < n) out[j] = from_float<TO>(__uint_as_float(v[j]));
+  }
+}
+
 // kAmn: W is contiguous along its own rows m, not along k (the product with W itself instead of its transpose).
-// kGather: X has a row per row of R, fetched four at a time by index; else a row per place.
+// kGather: X has a row per row of R, fetched by index; else a row per place.
+// Warps: 0 copies by tensor map, 1 matrix instructions, 2-5 results, 6-9 copies by index, 10 hands those over.
 template <bool kAmn, bool kGather, typename TO>
-__global__ void __launch_bounds__(192, 1) k_route_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                                                          const ProductArgs a) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192, 1)
+    k_route_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const ProductArgs a) {
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
   T5Block* b = reinterpret_cast<T5Block*>(stages + kStages * kStage);
   int* off = reinterpret_cast<int*>(b + 1);
   int* part = off + a.E + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  t5_begin(b, 4);
+  const u32 rank = cluster_rank();
+  t5_begin(b, kGather ? 3 : 1, 4);
   list_parts(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 63) / 64;
   const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
   zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
 
-  if (warp == 0) {  // copies
-    u32 it = 0;
-    bool ok = true;
-    for (i64 id = blockIdx.x; ok && id < n_tiles; id += gridDim.x) {
-      const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m0 = static_cast<int>(id % n_mt) * kTileM, n16 = (t.n + 15) & ~15;
-      int4 r[2];
-      if (kGather) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int g = (lane + 32 * h) * 4;
-          r[h].x = g + 0 < t.n ? a.rows[t.first + g + 0] : a.x_rows;
-          r[h].y = g + 1 < t.n ? a.rows[t.first + g + 1] : a.x_rows;
-          r[h].z = g + 2 < t.n ? a.rows[t.first + g + 2] : a.x_rows;
-          r[h].w = g + 3 < t.n ? a.rows[t.first + g + 3] : a.x_rows;
-        }
-      }
-      const u32 bytes = kStageA + (kGather ? n16 : (n16 + 31) / 32 * 32) * kRowBytes;
-      for (int kb = 0; kb < n_kb; ++kb, ++it) {
-        const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kStageA;
-        ok = t5_wait(&b->empty[s], ((it / kStages) & 1) ^ 1);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(&b->full[s], bytes);
-          if (kAmn) {
-            tma_load_3d(sa, &map_w, m0, kb * 64, t.e, &b->full[s]);
-            tma_load_3d(sa + kStageA / 2, &map_w, m0 + 64, kb * 64, t.e, &b->full[s]);
-          } else {
-            tma_load_3d(sa, &map_w, kb * 64, m0, t.e, &b->full[s]);
-          }
-        }
-        __syncwarp();
-        if (kGather) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            if ((lane + 32 * h) * 4 < n16) tma_gather4(sb + (lane + 32 * h) * 4 * kRowBytes, &map_x, kb * 64, r[h], &b->full[s]);
-        } else if (lane * 32 < n16) {
-          tma_load_2d(sb + lane * 32 * kRowBytes, &map_x, kb * 64, t.first + lane * 32, &b->full[s]);
-        }
-      }
-    }
-    if (!ok) {
-      if (lane == 0) dev_set_error(a.err, kDevTimeout);
-      t5_drain_copies(b, it);
-    }
-  } else if (warp == 1) {  // matrix instructions
-    if (lane == 0) {
+  if (warp == 0) {
+    copy_tiles<2, kAmn, kGather>(a, &map_w, &map_x, b, stage0, off, part, n_tiles, n_mt);
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
       u32 it = 0, n_done = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x; ok && id < n_tiles; id += gridDim.x, ++n_done) {
+      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1, ++n_done) {
         const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-        const u32 idesc = t5_idesc(a.type, kAmn, false, kTileM, (t.n + 15) & ~15), buf = n_done & 1, d = tmem + buf * kTileN;
+        const u32 idesc = t5_idesc(a.type, kAmn, false, kTileM, round32(t.n)), buf = n_done & 1, d = tmem + buf * kTileN;
         ok = t5_wait(&b->sums_empty[buf], ((n_done >> 1) & 1) ^ 1);
         if (!ok) break;
         t5_fence_after();
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
-          const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kStageA;
+          const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kHalf;
           ok = t5_wait(&b->full[s], (it / kStages) & 1);
           if (!ok) break;
           t5_fence_after();
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const u64 da = kAmn ? t5_desc_mn(sa + j * 16 * kRowBytes, kStageA / 2) : t5_desc_k(sa + j * 32);
+            const u64 da = kAmn ? t5_desc_mn(sa + j * 16 * kRowBytes, kHalf / 2) : t5_desc_k(sa + j * 32);
             t5_mma_f16(d, da, t5_desc_k(sb + j * 32), idesc, kb > 0 || j > 0);
           }
           t5_commit(&b->empty[s]);
@@ -223,18 +347,17 @@ __global__ void __launch_bounds__(192, 1) k_route_product(const __grid_constant_
       }
       if (!ok) {
         dev_set_error(a.err, kDevTimeout);
-        t5_commit(&b->drain);
-        t5_wait(&b->drain, 0);
+        t5_drain_matrix(b);
       }
     }
     __syncwarp();
-  } else {  // results
+  } else if (warp < 6) {
     const int quad = warp & 3;
     u32 n_done = 0;
     bool ok = true;
-    for (i64 id = blockIdx.x; ok && id < n_tiles; id += gridDim.x, ++n_done) {
+    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1, ++n_done) {
       const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m = static_cast<int>(id % n_mt) * kTileM + quad * 32 + lane;
+      const int m = static_cast<int>(id % n_mt) * kTileM + rank * 128 + quad * 32 + lane;
       const u32 buf = n_done & 1;
       ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done >> 1) & 1));
       if (!ok) break;
@@ -246,22 +369,26 @@ __global__ void __launch_bounds__(192, 1) k_route_product(const __grid_constant_
         store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + c, t.n - c, m, a.n_m, v);
       }
       t5_fence_before();
-      if (lane == 0) mbar_arrive(&b->sums_empty[buf]);
+      if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+  } else if (warp < 10) {
+    gather_rows<2>(a, b, stage0, off, part, n_tiles, n_mt, threadIdx.x - 192);
+  } else {
+    if (lane == 0) hand_over_rows(a, b, n_tiles, n_kb);
+    __syncwarp();
   }
-  t5_fence_before();
-  __syncthreads();
-  t5_fence_after();
-  if (warp == 0) tmem_free(tmem, kTmemColumns);
+  t5_end(tmem);
 }
 
 // 8 bits.  The sums of 128 values of k go to a buffer of their own in tensor memory; eight warps take them out, multiply by both
 // scales and add them up in registers (a thread: one row of W, half the places of the tile).
-// kRowScales: W has scales for each row and 128 values; else for each 128 rows, so that a tile has one.
+// kRowScales: W has scales for each row and 128 values; else for each 128 rows, so that a block's half of the tile has one.
+// Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 4-11 results.  The results' registers are what the others
+// give up: 512 threads begin with 128 each (384 with 168).
 template <bool kGather, bool kRowScales, typename TO>
-__global__ void __launch_bounds__(320, 1) k_route_product8(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                                                           const ProductArgs a) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384, 1)
+    k_route_product_scaled(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const ProductArgs a) {
   constexpr int kAhead = 4;  // blocks of k whose scales are brought in together
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
@@ -270,63 +397,26 @@ __global__ void __launch_bounds__(320, 1) k_route_product8(const __grid_constant
   int* off = reinterpret_cast<int*>(scale + 2 * kAhead * kTileN);
   int* part = off + a.E + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  t5_begin(b, 8);
+  const u32 rank = cluster_rank();
+  t5_begin(b, kGather ? 3 : 1, 8);
   list_parts(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 127) / 128;
   const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
   zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
 
-  if (warp == 0) {
-    u32 it = 0;
-    bool ok = true;
-    for (i64 id = blockIdx.x; ok && id < n_tiles; id += gridDim.x) {
-      const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m0 = static_cast<int>(id % n_mt) * kTileM, n16 = (t.n + 15) & ~15;
-      int4 r[2];
-      if (kGather) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int g = (lane + 32 * h) * 4;
-          r[h].x = g + 0 < t.n ? a.rows[t.first + g + 0] : a.x_rows;
-          r[h].y = g + 1 < t.n ? a.rows[t.first + g + 1] : a.x_rows;
-          r[h].z = g + 2 < t.n ? a.rows[t.first + g + 2] : a.x_rows;
-          r[h].w = g + 3 < t.n ? a.rows[t.first + g + 3] : a.x_rows;
-        }
-      }
-      const u32 bytes = kStageA + (kGather ? n16 : (n16 + 31) / 32 * 32) * kRowBytes;
-      for (int kb = 0; kb < n_kb; ++kb, ++it) {
-        const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kStageA;
-        ok = t5_wait(&b->empty[s], ((it / kStages) & 1) ^ 1);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(&b->full[s], bytes);
-          tma_load_3d(sa, &map_w, kb * 128, m0, t.e, &b->full[s]);
-        }
-        __syncwarp();
-        if (kGather) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            if ((lane + 32 * h) * 4 < n16) tma_gather4(sb + (lane + 32 * h) * 4 * kRowBytes, &map_x, kb * 128, r[h], &b->full[s]);
-        } else if (lane * 32 < n16) {
-          tma_load_2d(sb + lane * 32 * kRowBytes, &map_x, kb * 128, t.first + lane * 32, &b->full[s]);
-        }
-      }
-    }
-    if (!ok) {
-      if (lane == 0) dev_set_error(a.err, kDevTimeout);
-      t5_drain_copies(b, it);
-    }
-  } else if (warp == 1) {
-    if (lane == 0) {
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kGather ? 48 : 88));
+    if (warp == 0) {
+      copy_tiles<1, false, kGather>(a, &map_w, &map_x, b, stage0, off, part, n_tiles, n_mt);
+    } else if (warp == 1 && lane == 0 && rank == 0) {
       u32 it = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x; ok && id < n_tiles; id += gridDim.x) {
+      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
         const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-        const u32 idesc = t5_idesc(a.type, false, false, kTileM, (t.n + 15) & ~15);
+        const u32 idesc = t5_idesc(a.type, false, false, kTileM, round32(t.n));
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
-          const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kStageA, buf = it & 1, d = tmem + buf * kTileN;
+          const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kHalf, buf = it & 1, d = tmem + buf * kTileN;
           ok = t5_wait(&b->sums_empty[buf], ((it >> 1) & 1) ^ 1) && t5_wait(&b->full[s], (it / kStages) & 1);
           if (!ok) break;
           t5_fence_after();
@@ -338,19 +428,20 @@ __global__ void __launch_bounds__(320, 1) k_route_product8(const __grid_constant
       }
       if (!ok) {
         dev_set_error(a.err, kDevTimeout);
-        t5_commit(&b->drain);
-        t5_wait(&b->drain, 0);
+        t5_drain_matrix(b);
       }
     }
+    if (kGather && warp == 2 && lane == 0) hand_over_rows(a, b, n_tiles, n_kb);
     __syncwarp();
-  } else {
-    const int quad = warp & 3, half = (warp - 2) >> 2, tid = threadIdx.x - 64;
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(208));
+    const int quad = warp & 3, half = (warp - 4) >> 2, tid = threadIdx.x - 128;
     u32 it = 0;
     bool ok = true;
     // (a wait that gave up skips the work from there on, not the barriers among these warps)
-    for (i64 id = blockIdx.x; id < n_tiles; id += gridDim.x) {
+    for (i64 id = blockIdx.x >> 1; id < n_tiles; id += gridDim.x >> 1) {
       const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m0 = static_cast<int>(id % n_mt) * kTileM, m = m0 + quad * 32 + lane;
+      const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128, m = m0 + quad * 32 + lane;
       float acc[4][32];
 #pragma unroll
       for (int c = 0; c < 4; ++c)
@@ -359,7 +450,8 @@ __global__ void __launch_bounds__(320, 1) k_route_product8(const __grid_constant
       // this thread brings in the scales of place `tid` of the tile
       const float* xs = nullptr;
       if (tid < t.n) xs = a.xs + static_cast<i64>(kGather ? a.rows[t.first + tid] : t.first + tid) * a.xs_stride;
-      const float* ws = a.ws + static_cast<i64>(t.e) * a.ws_block + (kRowScales ? static_cast<i64>(min(m, a.n_m - 1)) : static_cast<i64>(m0 / 128)) * a.ws_row;
+      const float* ws = a.ws + static_cast<i64>(t.e) * a.ws_block +
+                        (kRowScales ? static_cast<i64>(min(m, a.n_m - 1)) : static_cast<i64>(min(m0, a.n_m - 1) / 128)) * a.ws_row;
       float next[kAhead], wnext[kAhead];
       auto fetch = [&](int kb) {
 #pragma unroll
@@ -404,7 +496,7 @@ __global__ void __launch_bounds__(320, 1) k_route_product8(const __grid_constant
                 }
               }
               t5_fence_before();
-              if (lane == 0) mbar_arrive(&b->sums_empty[buf]);
+              if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
               ++it;
             }
           }
@@ -423,76 +515,53 @@ __global__ void __launch_bounds__(320, 1) k_route_product8(const __grid_constant
       asm volatile("bar.sync 1, 256;" ::: "memory");  // (the scales' buffers go round again)
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(48));
+    gather_rows<1>(a, b, stage0, off, part, n_tiles, n_mt, threadIdx.x - 384);
   }
-  t5_fence_before();
-  __syncthreads();
-  t5_fence_after();
-  if (warp == 0) tmem_free(tmem, kTmemColumns);
+  t5_end(tmem);
 }
 
-// Both operands lie with the reduction across their rows; rows come four at a time by index, and an index behind the last row reads
-// as zeros, which ends a column's sum inside a stage whatever lies behind it.
+// Both operands lie with the reduction (64 places a stage) across their rows and come by index, 16 bytes at a time: what lies behind a
+// column's last place is not read but zero, so that a sum ends inside a stage whatever its neighbour holds.
+// Warps: 0 hands over what 6-9 copy, 1 matrix instructions, 2-5 results.
 template <bool kGather, typename TO>
-__global__ void __launch_bounds__(192, 1) k_route_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x,
-                                                     const DwArgs a) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(320, 1) k_route_dw(const DwArgs a) {
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
   T5Block* b = reinterpret_cast<T5Block*>(stages + kStages * kStage);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  t5_begin(b, 4);
-  const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_jt = (a.n_j + kTileN - 1) / kTileN;
-  const i64 n_tiles = static_cast<i64>(a.E) * n_mt * n_jt;
+  const u32 rank = cluster_rank();
+  t5_begin(b, 2, 4);
+  const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_jt = (a.n_j + kTileN - 1) / kTileN, n_per = n_mt * n_jt;
+  const i64 n_tiles = static_cast<i64>(a.E) * n_per;
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
   constexpr u32 kBlock = 64 * kRowBytes;  // 64 places of 64 values
 
   if (warp == 0) {
-    u32 it = 0;
-    bool ok = true;
-    const int g = lane & 15, hi = lane >> 4;
-    for (i64 id = blockIdx.x; ok && id < n_tiles; id += gridDim.x) {
-      const int e = static_cast<int>(id / (n_mt * n_jt)), rest = static_cast<int>(id % (n_mt * n_jt));
-      const int m0 = rest % n_mt * kTileM, j0 = rest / n_mt * kTileN, n_cb = min(4, (a.n_j - j0 + 63) / 64);
-      const int p0 = static_cast<int>(a.offsets[e]), p1 = static_cast<int>(a.offsets[e + 1]);
-      const u32 bytes = (2 + n_cb) * kBlock;
-      const int none = static_cast<int>(a.places);
-      auto row = [&](int p) { return p < p1 ? (kGather ? a.rows[p] : p) : a.x_rows; };
-      int4 next = make_int4(row(p0 + 4 * g), row(p0 + 4 * g + 1), row(p0 + 4 * g + 2), row(p0 + 4 * g + 3));
-      for (int p = p0; p < p1; p += 64, ++it) {
-        const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kStageA;
-        const int q = p + 4 * g;
-        const int4 rx = next, rp = make_int4(q < p1 ? q : none, q + 1 < p1 ? q + 1 : none, q + 2 < p1 ? q + 2 : none, q + 3 < p1 ? q + 3 : none);
-        next = make_int4(row(q + 64), row(q + 65), row(q + 66), row(q + 67));
-        ok = t5_wait(&b->empty[s], ((it / kStages) & 1) ^ 1);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane == 0) mbar_arrive_expect_tx(&b->full[s], bytes);
-        __syncwarp();
-        tma_gather4(sa + hi * kBlock + g * 4 * kRowBytes, &map_p, m0 + hi * 64, rp, &b->full[s]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int cb = 2 * h + hi;
-          if (cb < n_cb) tma_gather4(sb + cb * kBlock + g * 4 * kRowBytes, &map_x, j0 + cb * 64, rx, &b->full[s]);
-        }
+    if (lane == 0) {
+      u32 it = 0;
+      bool ok = true;
+      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+        const int e = static_cast<int>(id / n_per), n_st = (static_cast<int>(a.offsets[e + 1] - a.offsets[e]) + 63) / 64;
+        for (int i = 0; ok && i < n_st; ++i, ++it) ok = hand_over(b, it);
       }
-    }
-    if (!ok) {
-      if (lane == 0) dev_set_error(a.err, kDevTimeout);
-      t5_drain_copies(b, it);
+      if (!ok) dev_set_error(a.err, kDevTimeout);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
       u32 it = 0, n_done = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x; ok && id < n_tiles; id += gridDim.x) {
-        const int e = static_cast<int>(id / (n_mt * n_jt)), rest = static_cast<int>(id % (n_mt * n_jt)), j0 = rest / n_mt * kTileN;
+      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+        const int e = static_cast<int>(id / n_per), j0 = static_cast<int>(id % n_per) / n_mt * kTileN;
         const int p0 = static_cast<int>(a.offsets[e]), p1 = static_cast<int>(a.offsets[e + 1]);
         if (p0 >= p1) continue;
-        const u32 idesc = t5_idesc(a.type, true, true, kTileM, (min(kTileN, a.n_j - j0) + 15) & ~15), buf = n_done & 1, d = tmem + buf * kTileN;
+        const u32 idesc = t5_idesc(a.type, true, true, kTileM, a.n_j - j0 > 128 ? 256 : 128), buf = n_done & 1, d = tmem + buf * kTileN;
         ok = t5_wait(&b->sums_empty[buf], ((n_done >> 1) & 1) ^ 1);
         if (!ok) break;
         t5_fence_after();
         for (int p = p0; p < p1; p += 64, ++it) {
-          const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kStageA;
+          const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kHalf;
           ok = t5_wait(&b->full[s], (it / kStages) & 1);
           if (!ok) break;
           t5_fence_after();
@@ -506,56 +575,98 @@ __global__ void __launch_bounds__(192, 1) k_route_dw(const __grid_constant__ CUt
       }
       if (!ok) {
         dev_set_error(a.err, kDevTimeout);
-        t5_commit(&b->drain);
-        t5_wait(&b->drain, 0);
+        t5_drain_matrix(b);
       }
     }
     __syncwarp();
-  } else {
+  } else if (warp >= 6) {
+    // sixteen lanes have a row: 256 bytes of dP, 256 (or 128) of X
+    const int thread = threadIdx.x - 192, c = thread & 15, r0 = thread >> 4;
+    const u32 at = (c >> 3) * kBlock + r0 * kRowBytes + (((c & 7) ^ r0) << 4);  // (rows r0 + 8 i: the same swizzle)
+    CopyQueue queue(b);
+    bool ok = true;
+    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+      const int e = static_cast<int>(id / n_per), rest = static_cast<int>(id % n_per);
+      const int j0 = rest / n_mt * kTileN, half = a.n_j - j0 > 128 ? 128 : 64;
+      const int m = rest % n_mt * kTileM + rank * 128 + c * 8, j = j0 + rank * half + c * 8;
+      const int p0 = static_cast<int>(a.offsets[e]), p1 = static_cast<int>(a.offsets[e + 1]);
+      const u32 m_bytes = 2 * max(0, min(8, a.n_m - m)), j_bytes = 2 * max(0, min(8, a.n_j - j));
+      const char* dp = a.dp + (m_bytes ? 2 * static_cast<i64>(m) : 0);
+      const char* x = a.x + (j_bytes ? 2 * static_cast<i64>(j) : 0);
+      int next[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int q = p0 + r0 + 8 * i;
+        next[i] = q < p1 ? (kGather ? a.rows[q] : q) : -1;
+      }
+      for (int p = p0; p < p1; p += 64) {
+        ok = queue.slot_free();
+        if (!ok) break;
+        const u32 dst = stage0 + queue.issued % kStages * kStage + at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int q = p + r0 + 8 * i;
+          copy16(dst + i * 8 * kRowBytes, q < p1 ? dp + q * a.dp_stride : dp, q < p1 ? m_bytes : 0);
+        }
+        if (c * 8 < half) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            copy16(dst + kHalf + i * 8 * kRowBytes, next[i] >= 0 ? x + next[i] * a.x_stride : x, next[i] >= 0 ? j_bytes : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int q = p + 64 + r0 + 8 * i;
+          next[i] = q < p1 ? (kGather ? a.rows[q] : q) : -1;
+        }
+        queue.done();
+      }
+    }
+    copy_wait_all();
+    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+  } else if (warp >= 2) {
     const int quad = warp & 3;
     u32 n_done = 0;
     bool ok = true;
-    for (i64 id = blockIdx.x; ok && id < n_tiles; id += gridDim.x) {
-      const int e = static_cast<int>(id / (n_mt * n_jt)), rest = static_cast<int>(id % (n_mt * n_jt));
-      const int m = rest % n_mt * kTileM + quad * 32 + lane, j0 = rest / n_mt * kTileN, n = min(kTileN, a.n_j - j0);
+    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+      const int e = static_cast<int>(id / n_per), rest = static_cast<int>(id % n_per);
+      const int m = rest % n_mt * kTileM + rank * 128 + quad * 32 + lane, j0 = rest / n_mt * kTileN, n = min(kTileN, a.n_j - j0);
       const bool some = a.offsets[e] < a.offsets[e + 1];
-      TO* out = static_cast<TO*>(a.out) + static_cast<i64>(e) * a.out_block + static_cast<i64>(m) * a.out_stride + j0;
+      TO* out = static_cast<TO*>(a.out) + static_cast<i64>(e) * a.out_block + static_cast<i64>(m - lane) * a.out_stride + j0;
       const u32 buf = n_done & 1;
       if (some) {
         ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done >> 1) & 1));
         if (!ok) break;
         t5_fence_after();
-      }
-      for (int c = 0; c < n; c += 32) {
-        u32 v[32];
-        if (some) {
+        for (int c = 0; c < n; c += 32) {
+          u32 v[32];
           t5_ld32(v, tmem + buf * kTileN + c + (static_cast<u32>(quad * 32) << 16));
           t5_wait_ld();
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0;
+          if (m < a.n_m) store_run(out + lane * a.out_stride + c, n - c, a.out_align, v);
         }
-        if (m < a.n_m) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (c + j < n) out[c + j] = from_float<TO>(__uint_as_float(v[j]));
-        }
+      } else {  // a column without entries
+        for (int r = 0; r < 32 && m - lane + r < a.n_m; ++r)
+          if (a.out_align >= 16) {
+            for (int c = lane * 8; c < n; c += 256)
+              for (int j = 0; j < 8 * static_cast<int>(sizeof(TO)) / 16; ++j)
+                if (c + 8 <= n) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(out + r * a.out_stride + c) + 16 * j) = make_uint4(0, 0, 0, 0);
+            for (int c = n / 8 * 8 + lane; c < n; c += 32) out[r * a.out_stride + c] = from_float<TO>(0.f);
+          } else {
+            for (int c = lane; c < n; c += 32) out[r * a.out_stride + c] = from_float<TO>(0.f);
+          }
       }
       if (some) {
         t5_fence_before();
-        if (lane == 0) mbar_arrive(&b->sums_empty[buf]);
+        if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
         ++n_done;
       }
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   }
-  t5_fence_before();
-  __syncthreads();
-  t5_fence_after();
-  if (warp == 0) tmem_free(tmem, kTmemColumns);
+  __syncwarp();
+  t5_end(tmem);
 }
 
-// Copies into an aligned layout for the tensor maps: dst (blocks x rows x padded columns), the padding zero.
+// Copies into an aligned layout: dst (blocks x rows x padded columns), the padding zero.
 template <typename T>
 __global__ void k_route_pack(const T* __restrict__ src, i64 block_stride, i64 row_stride, i64 col_stride, i64 n_blocks, i64 n_rows,
                              i64 n_cols, i64 padded, T* __restrict__ dst) {

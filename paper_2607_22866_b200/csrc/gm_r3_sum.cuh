@@ -71,6 +71,23 @@ __device__ __forceinline__ void store_cols(T* p, const float (&v)[8]) {
   else *p = from_float<T>(v[0]);
 }
 
+// A thread's columns as they lie in memory, so that many loads can be under way in few registers.
+template <typename T, bool kVec> struct Raw {
+  using type = T;
+  static __device__ __forceinline__ type load(const T* p) { return *p; }
+  static __device__ __forceinline__ void values(const type& r, float (&v)[8]) { v[0] = static_cast<float>(r); }
+};
+template <typename T> struct Raw<T, true> {
+  struct alignas(16) type { T v[8]; };
+  static __device__ __forceinline__ type load(const T* p) {
+    type r;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(type) / 16); ++i) reinterpret_cast<uint4*>(&r)[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    return r;
+  }
+  static __device__ __forceinline__ void values(const type& r, float (&v)[8]) { Vec8<T>::load(r.v, v); }
+};
+
 struct SumArgs {
   const i64* row_ptr;
   const float* val;       // nullptr: every entry counts once
@@ -99,25 +116,27 @@ __global__ void __launch_bounds__(kSumThreads) k_route_sum(const SumArgs a, int 
   const int routed = static_cast<int>(a.offsets[a.E]);
   const TI* p = static_cast<const TI*>(a.p) + c;
   float acc[8] = {};
-  for (i64 q = q0; q < q1; q += 4) {  // four rows in flight
-    float v[4][8], r[4];
+  for (i64 q = q0; q < q1; q += 8) {  // eight rows in flight: their places first, then their values, then the sums
+    int at[8];
+    float r[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      r[j] = 0.f;
-#pragma unroll
-      for (int x = 0; x < 8; ++x) v[j][x] = 0.f;
-      if (q + j < q1) {
-        const int at = a.pos[q + j];
-        if (at < routed) {
-          r[j] = a.val ? a.val[q + j] : 1.f;
-          load_cols<TI, kVec>(p + at * a.p_stride, v[j]);
-        }
-      }
+    for (int j = 0; j < 8; ++j) {
+      const bool in = q + j < q1;
+      at[j] = in ? a.pos[q + j] : INT_MAX;
+      r[j] = in && a.val ? a.val[q + j] : 1.f;
     }
+    typename Raw<TI, kVec>::type v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 8; ++j)
+      if (at[j] < routed) v[j] = Raw<TI, kVec>::load(p + at[j] * a.p_stride);
 #pragma unroll
-      for (int x = 0; x < kCols; ++x) acc[x] = fmaf(r[j], v[j][x], acc[x]);
+    for (int j = 0; j < 8; ++j)
+      if (at[j] < routed) {
+        float f[8];
+        Raw<TI, kVec>::values(v[j], f);
+#pragma unroll
+        for (int x = 0; x < kCols; ++x) acc[x] = fmaf(r[j], f[x], acc[x]);
+      }
   }
   store_cols<TO, kVec>(static_cast<TO*>(a.y) + i * a.y_stride + c, acc);
 }

@@ -146,13 +146,20 @@ static int contiguous_rows(gm_dense* M, Scratch* mem) {
   return pack(gm_dense(*M), mem, num_sms, M);
 }
 
-// A map of rows: `box_rows` at a time (1: for loads of four rows by index).
-static int map_rows(CUtensorMap* map, gm_dense M, uint32_t box_rows, Scratch* mem, int num_sms) {
+// Rows that start on 16 bytes: as they are, or copied.
+static int aligned_rows(gm_dense* M, Scratch* mem, int num_sms) {
+  const i64 es = static_cast<i64>(elem_size(M->dtype));
+  const bool fits = reinterpret_cast<uintptr_t>(M->data) % 16 == 0 && (M->col_stride == 1 || M->n_cols <= 1) && (M->n_rows <= 1 || M->row_stride * es % 16 == 0);
+  return fits ? GM_OK : pack(gm_dense(*M), mem, num_sms, M);
+}
+
+// A map of rows, 32 at a time.
+static int map_rows(CUtensorMap* map, gm_dense M, Scratch* mem, int num_sms) {
   if (!map_fits(M, false)) GM_TRY(pack(gm_dense(M), mem, num_sms, &M));
   const i64 es = static_cast<i64>(elem_size(M.dtype));
   const uint64_t dims[2] = {static_cast<uint64_t>(M.n_cols), static_cast<uint64_t>(M.n_rows)};
   const uint64_t strides[1] = {static_cast<uint64_t>(M.n_rows > 1 ? M.row_stride * es : (M.n_cols * es + 15) / 16 * 16)};
-  const uint32_t box[2] = {static_cast<uint32_t>(kRowBytes / es), box_rows};
+  const uint32_t box[2] = {static_cast<uint32_t>(kRowBytes / es), 32};
   return make_map(map, M.dtype, 2, M.data, dims, strides, box);
 }
 
@@ -183,10 +190,11 @@ static int zero_out(const gm_dense& M, cudaStream_t st) {
   return GM_OK;
 }
 
-template <typename K>
-static int launch_t5(K kernel, i64 tiles, int num_sms, int threads, size_t smem, cudaStream_t st, const CUtensorMap& m0, const CUtensorMap& m1, const auto& args) {
+// A pair of blocks per tile, at most one pair per two SMs.
+template <typename... A>
+static int launch_t5(void (*kernel)(A...), i64 tiles, int num_sms, int threads, size_t smem, cudaStream_t st, const A&... args) {
   GM_TRY(set_smem(reinterpret_cast<const void*>(kernel), smem));
-  kernel<<<static_cast<unsigned>(std::max<i64>(1, std::min<i64>(tiles, num_sms))), threads, smem, st>>>(m0, m1, args);
+  kernel<<<static_cast<unsigned>(2 * std::max<i64>(1, std::min<i64>(tiles, num_sms / 2))), threads, smem, st>>>(args...);
   GM_CUDA(cudaGetLastError());
   return GM_OK;
 }
@@ -225,16 +233,23 @@ static int product(const gm_route* r, const gm_dense& X, bool by_entry, const gm
   const uint64_t row_bytes = static_cast<uint64_t>(outer > 1 ? outer_stride * es : (inner * es + 15) / 16 * 16);
   const uint64_t dims[3] = {static_cast<uint64_t>(inner), static_cast<uint64_t>(outer), static_cast<uint64_t>(V.n_blocks)};
   const uint64_t strides[2] = {row_bytes, V.n_blocks > 1 ? static_cast<uint64_t>(V.block_stride * es) : row_bytes * outer};
-  const uint32_t box[3] = {64, m_inner ? 64u : static_cast<uint32_t>(kTileM), 1};
+  const uint32_t box[3] = {64, m_inner ? 64u : 128u, 1};
   GM_TRY(make_map(&map_w, V.dtype, 3, V.data, dims, strides, box));
-  GM_TRY(map_rows(&map_x, X, by_entry ? 32 : 1, &mem, num_sms));
+  gm_dense rows = X;
+  if (by_entry) {
+    GM_TRY(map_rows(&map_x, X, &mem, num_sms));
+  } else {
+    GM_TRY(aligned_rows(&rows, &mem, num_sms));
+    map_x = map_w;  // (not used)
+  }
   ProductArgs a = {};
   a.offsets = r->offsets;
   a.rows = r->rows;
   a.E = r->E;
   a.n_m = static_cast<int>(n_m);
   a.n_k = static_cast<int>(n_k);
-  a.x_rows = static_cast<int>(X.n_rows);
+  a.x = static_cast<const char*>(rows.data);
+  a.x_stride = rows.row_stride * es;
   a.places = r->nnz;
   a.out = out.data;
   a.out_stride = out.row_stride;
@@ -242,7 +257,7 @@ static int product(const gm_route* r, const gm_dense& X, bool by_entry, const gm
   a.err = r->err;
   const i64 tiles = ((r->nnz + kTileN - 1) / kTileN + std::min<i64>(r->E, r->nnz)) * ((n_m + kTileM - 1) / kTileM);
   const size_t smem = product_smem(r->E, false);
-  const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, 192, smem, st, map_w, map_x, a); };
+  const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, by_entry ? 192 : 352, smem, st, map_w, map_x, a); };
   const auto typed = [&](auto* tag) {
     using TO = std::remove_pointer_t<decltype(tag)>;
     if (m_inner) return by_entry ? go(k_route_product<true, false, TO>) : go(k_route_product<true, true, TO>);
@@ -465,24 +480,30 @@ int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dens
     int num_sms, smem_optin;
     GM_TRY(device_facts_basic(&num_sms, &smem_optin));
     Scratch mem(st);
-    CUtensorMap map_p, map_x;
-    GM_TRY(map_rows(&map_p, *dP, 1, &mem, num_sms));
-    GM_TRY(map_rows(&map_x, *X, 1, &mem, num_sms));
+    gm_dense G = *dP, V = *X;
+    GM_TRY(aligned_rows(&G, &mem, num_sms));
+    GM_TRY(aligned_rows(&V, &mem, num_sms));
     DwArgs a = {};
     a.offsets = route->offsets;
-    a.rows = by_entry ? nullptr : route->rows;
+    a.rows = route->rows;
     a.E = route->E;
     a.n_m = static_cast<int>(dP->n_cols);
     a.n_j = static_cast<int>(X->n_cols);
-    a.x_rows = static_cast<int>(X->n_rows);
-    a.places = route->nnz;
+    a.dp = static_cast<const char*>(G.data);
+    a.dp_stride = G.row_stride * 2;
+    a.x = static_cast<const char*>(V.data);
+    a.x_stride = V.row_stride * 2;
     a.out = dW->data;
     a.out_block = dW->block_stride;
     a.out_stride = dW->row_stride;
+    const i64 oes = static_cast<i64>(elem_size(dW->dtype));
+    for (a.out_align = 32; a.out_align > 8; a.out_align /= 2)
+      if (reinterpret_cast<uintptr_t>(dW->data) % a.out_align == 0 && (dW->n_rows <= 1 || dW->row_stride * oes % a.out_align == 0) &&
+          (dW->n_blocks <= 1 || dW->block_stride * oes % a.out_align == 0)) break;
     a.type = dP->dtype == GM_BF16 ? 1 : 0;
     a.err = route->err;
     const i64 tiles = static_cast<i64>(a.E) * ((a.n_m + kTileM - 1) / kTileM) * ((a.n_j + kTileN - 1) / kTileN);
-    const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, 192, kT5Smem, st, map_p, map_x, a); };
+    const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, 320, kT5Smem, st, a); };
     switch (dW->dtype) {
       case GM_F32: return by_entry ? go(k_route_dw<false, float>) : go(k_route_dw<true, float>);
       case GM_BF16: return by_entry ? go(k_route_dw<false, __nv_bfloat16>) : go(k_route_dw<true, __nv_bfloat16>);
@@ -578,15 +599,16 @@ int gm_block_quantize(const gm_dense* X, int block_rows, const gm_dense* Q, cons
     a.n_rows = X->n_rows;
     a.n_cols = static_cast<int>(X->n_cols);
     a.col_groups = static_cast<int>(cg);
-    a.q = static_cast<u32*>(Q->data);
+    a.q = static_cast<unsigned char*>(Q->data);
     a.s = static_cast<float*>(S->data);
     const bool vec = X->col_stride == 1 && rows_aligned(*X) && (X->n_blocks <= 1 || X->block_stride % 8 == 0) && reinterpret_cast<uintptr_t>(Q->data) % 8 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const i64 units = X->n_blocks * rg * cg, blocks = block_rows == 1 ? (units + 15) / 16 : units;
+    const bool flat = vec && X->n_cols % 128 == 0 && (X->n_rows <= 1 || X->row_stride == X->n_cols) && (X->n_blocks <= 1 || X->block_stride == X->n_rows * X->n_cols);
+    const i64 units = X->n_blocks * rg * cg, blocks = block_rows == 1 ? (units + 16 * kQuantAhead - 1) / (16 * kQuantAhead) : units;
     GM_TRY(sum_grid(blocks, "quantize"));
     const auto typed = [&](auto* tag) {
       using T = std::remove_pointer_t<decltype(tag)>;
-      if (block_rows == 1) (vec ? k_quantize_rows<T, true> : k_quantize_rows<T, false>)<<<static_cast<unsigned>(blocks), 256, 0, st>>>(a);
+      if (block_rows == 1) (flat ? k_quantize_rows<T, true, true> : vec ? k_quantize_rows<T, true, false> : k_quantize_rows<T, false, false>)<<<static_cast<unsigned>(blocks), 256, 0, st>>>(a);
       else (vec ? k_quantize_tiles<T, true> : k_quantize_tiles<T, false>)<<<static_cast<unsigned>(blocks), 256, 0, st>>>(a, static_cast<int>(rg));
       GM_CUDA(cudaGetLastError());
       return static_cast<int>(GM_OK);
@@ -628,16 +650,23 @@ int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_
     const uint64_t row_bytes = static_cast<uint64_t>(V.n_rows > 1 ? V.row_stride : (V.n_cols + 15) / 16 * 16);
     const uint64_t dims[3] = {static_cast<uint64_t>(V.n_cols), static_cast<uint64_t>(V.n_rows), static_cast<uint64_t>(V.n_blocks)};
     const uint64_t strides[2] = {row_bytes, V.n_blocks > 1 ? static_cast<uint64_t>(V.block_stride) : row_bytes * V.n_rows};
-    const uint32_t box[3] = {kRowBytes, kTileM, 1};
+    const uint32_t box[3] = {kRowBytes, 128, 1};
     GM_TRY(make_map(&map_w, GM_E4M3, 3, V.data, dims, strides, box));
-    GM_TRY(map_rows(&map_x, *Xq, by_entry ? 32 : 1, &mem, num_sms));
+    gm_dense rows = *Xq;
+    if (by_entry) {
+      GM_TRY(map_rows(&map_x, rows, &mem, num_sms));
+    } else {
+      GM_TRY(aligned_rows(&rows, &mem, num_sms));
+      map_x = map_w;  // (not used)
+    }
     ProductArgs a = {};
     a.offsets = route->offsets;
     a.rows = route->rows;
     a.E = route->E;
     a.n_m = static_cast<int>(Wq->n_rows);
     a.n_k = static_cast<int>(Wq->n_cols);
-    a.x_rows = static_cast<int>(Xq->n_rows);
+    a.x = static_cast<const char*>(rows.data);
+    a.x_stride = rows.row_stride;
     a.places = route->nnz;
     a.out = P->data;
     a.out_stride = P->row_stride;
@@ -650,11 +679,11 @@ int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_
     a.err = route->err;
     const i64 tiles = ((route->nnz + kTileN - 1) / kTileN + std::min<i64>(route->E, route->nnz)) * ((a.n_m + kTileM - 1) / kTileM);
     const size_t smem = product_smem(route->E, true);
-    const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, 320, smem, st, map_w, map_x, a); };
+    const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, by_entry ? 384 : 512, smem, st, map_w, map_x, a); };
     const auto typed = [&](auto* tag) {
       using TO = std::remove_pointer_t<decltype(tag)>;
-      if (row_scales) return by_entry ? go(k_route_product8<false, true, TO>) : go(k_route_product8<true, true, TO>);
-      return by_entry ? go(k_route_product8<false, false, TO>) : go(k_route_product8<true, false, TO>);
+      if (row_scales) return by_entry ? go(k_route_product_scaled<false, true, TO>) : go(k_route_product_scaled<true, true, TO>);
+      return by_entry ? go(k_route_product_scaled<false, false, TO>) : go(k_route_product_scaled<true, false, TO>);
     };
     switch (P->dtype) {
       case GM_F32: return typed(static_cast<float*>(nullptr));
