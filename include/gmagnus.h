@@ -334,13 +334,14 @@ typedef struct gm_route gm_route; /* opaque, owned by the library */
 #define GM_ROUTE_MAX_COLS 2048
 
 /* Puts the entries of R in the order of their columns (a stable counting sort).  R: f32 values, at most
- * GM_ROUTE_MAX_COLS columns (else GM_ERR_CAPACITY).  The route borrows R's row_ptr and vals (read by gm_route_sum
- * and its gradients, so values may change in between); col_idx is read by this call's kernel only.  A route can be used
- * on other streams than the one it was made on when the caller orders them behind it, by any number of calls at a time. */
-int gm_route_plan(const gm_csr* R, void* cuda_stream, gm_route** route_out);
-/* Device arrays of the route, valid until it is destroyed: offsets (E + 1), and for every place its row of R and its entry;
- * pos: the place of every entry. */
-int gm_route_arrays(const gm_route* route, const int64_t** offsets, const int32_t** rows, const int32_t** order, const int32_t** pos);
+ * GM_ROUTE_MAX_COLS columns (else GM_ERR_CAPACITY).  The call writes the caller's device arrays
+ *   offsets      E + 1: first place of every column, and behind the last one the number of routed entries
+ *   rows, order  nnz: row of R and entry of R at every place
+ *   pos          nnz: place of every entry
+ * which the route borrows, like R's row_ptr and vals (read by gm_route_sum and its gradients, so values may change in
+ * between); col_idx is read by this call's kernel only.  A route can be used on other streams than the one it was made on when
+ * the caller orders them behind it, by any number of calls at a time. */
+int gm_route_plan(const gm_csr* R, int64_t* offsets, int32_t* rows, int32_t* order, int32_t* pos, void* cuda_stream, gm_route** route_out);
 /* GM_ERR_TIMEOUT when a kernel of an earlier call on this route gave up a wait (its results are then not valid), as
  * every further call on it does; GM_OK otherwise.  Does not wait: synchronise first to know about all of them. */
 int gm_route_status(const gm_route* route);

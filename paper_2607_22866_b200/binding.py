@@ -21,7 +21,7 @@ GM_MAX_LEVELS = 8
 EXPORTED_SYMBOLS = [
     "gm_set_allocator", "gm_planner_params", "gm_planner_batches", "gm_spgemm_plan", "gm_spgemm_plan_ex", "gm_spgemm_execute",
     "gm_spgemm_host", "gm_plan_get_info", "gm_exec_get_stats", "gm_plan_set_timing",
-    "gm_plan_get_row_products", "gm_row_products_noalloc", "gm_route_plan", "gm_route_arrays", "gm_route_status",
+    "gm_plan_get_row_products", "gm_row_products_noalloc", "gm_route_plan", "gm_route_status",
     "gm_route_destroy", "gm_route_product", "gm_route_product_dx", "gm_route_product_dw", "gm_route_sum",
     "gm_route_sum_grads", "gm_block_quantize", "gm_route_product_scaled", "gm_csr_free", "gm_plan_destroy", "gm_status_string", "gm_last_error",
 ]
@@ -139,8 +139,7 @@ def load_library(install_torch_allocator: bool = True):
         lib.gm_plan_get_row_products.argtypes = [vp, vp, vp]
         lib.gm_row_products_noalloc.argtypes = [P(_CSR), P(_CSR), vp, vp]
         D = P(_Dense)
-        lib.gm_route_plan.argtypes = [P(_CSR), vp, P(vp)]
-        lib.gm_route_arrays.argtypes = [vp, P(vp), P(vp), P(vp), P(vp)]
+        lib.gm_route_plan.argtypes = [P(_CSR), vp, vp, vp, vp, vp, P(vp)]
         lib.gm_route_status.argtypes = [vp]
         lib.gm_route_destroy.argtypes = [vp]
         lib.gm_route_destroy.restype = None
@@ -343,98 +342,84 @@ def spgemm_host(A, B, out_row_ptr: np.ndarray, out_col: np.ndarray, out_val: np.
 
 # ---------------------------------------------------------------------------------------------------------------------
 # Routed products: R (DeviceCSR) picks blocks of a dense factor.  No autograd graph is recorded; gradients have calls of their own.
+# (Marshalling is kept short here: a product of a few rows takes the GPU about as long as it takes the host to call it.)
 # ---------------------------------------------------------------------------------------------------------------------
 _DTYPES = {torch.float32: 0, torch.float64: 1, torch.bfloat16: 2, torch.float16: 3, torch.float8_e4m3fn: 4}
+_byref = ctypes.byref
 
 
 def _dense(t: torch.Tensor, where: str, device: torch.device) -> _Dense:
     if t.device != device:
         raise GmError(-1, where, f"a tensor on {t.device}, the others on {device}")
-    if t.dim() == 2:
-        (r, c), (rs, cs) = t.shape, t.stride()
-        b, bs = 1, 0
-    elif t.dim() == 3:
-        (b, r, c), (bs, rs, cs) = t.shape, t.stride()
-    else:
-        raise GmError(-1, where, f"a tensor of {t.dim()} dimensions: 2 or 3 expected")
-    return _Dense(t.data_ptr(), b, r, c, bs, rs, cs, _DTYPES.get(t.dtype, -1), 0)
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        return _Dense(t.data_ptr(), 1, shape[0], shape[1], 0, stride[0], stride[1], _DTYPES.get(t.dtype, -1), 0)
+    return _Dense(t.data_ptr(), *shape, *stride, _DTYPES.get(t.dtype, -1), 0)
 
 
-class _On:
-    """The device of a call's tensors, and the stream it was given, made current: what the call allocates belongs to that stream."""
+def _result(t: torch.Tensor) -> _Dense:
+    """A contiguous matrix that the call has just made."""
+    rows, cols = t.shape
+    return _Dense(t.data_ptr(), 1, rows, cols, 0, cols, 1, _DTYPES.get(t.dtype, -1), 0)
 
-    def __init__(self, where: str, device: torch.device, stream, tensors):
-        if device.type != "cuda":
-            raise GmError(-1, where, f"tensors on {device}: a CUDA device expected")
-        self._device = self._stream = None
-        if device.index != torch.cuda.current_device():
-            self._device = torch.cuda.device(device)
-        if stream is not None and stream != torch.cuda.current_stream(device):
-            self._stream = torch.cuda.stream(stream)
-            for t in tensors:  # their memory is not given to others before this stream is done with it
-                t.record_stream(stream)
 
-    def __enter__(self):
-        if self._device is not None:
-            self._device.__enter__()
-        if self._stream is not None:
-            self._stream.__enter__()
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+def _dims(t: torch.Tensor, where: str, name: str, dims: int):
+    if t.dim() != dims:
+        raise GmError(-2, where, f"{name}: {t.dim()} dimensions instead of {dims}")
 
-    def __exit__(self, *exc):
-        if self._stream is not None:
-            self._stream.__exit__(*exc)
-        if self._device is not None:
-            self._device.__exit__(*exc)
-        return False
+
+def _is_here(where: str, device: torch.device, stream) -> bool:
+    """Whether the call can run as it is: on the current device, on its current stream."""
+    if device.type != "cuda":
+        raise GmError(-1, where, f"tensors on {device}: a CUDA device expected")
+    return stream is None and device.index == torch._C._cuda_getDevice()
+
+
+def _there(call, device: torch.device, stream, *args, **kwargs):
+    """The same call with the tensors' device and the given stream made current, so that what it allocates belongs to that stream; the
+    inputs' memory is not given to others before the stream is done with it."""
+    with torch.cuda.device(device), torch.cuda.stream(stream):
+        if stream is not None:
+            for t in args:
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(stream)
+        return call(*args, **kwargs)
 
 
 class Route:
-    """Owner of a gm_route*: the entries of R in the order of their columns.  Keeps R alive, whose row_ptr and val it borrows."""
+    """Owner of a gm_route*: the entries of R in the order of their columns.
 
-    def __init__(self, handle, R: DeviceCSR, stream: int):
-        self._h, self.R, self._stream = handle, R, stream
-        self.n_rows, self.n_cols, self.nnz, self.device = R.n_rows, R.n_cols, R.nnz, R.row_ptr.device
-        ptrs = [ctypes.c_void_p() for _ in range(4)]
-        _check(load_library().gm_route_arrays(handle, *(ctypes.byref(p) for p in ptrs)), "gm_route_arrays")
-        self._ptrs = [p.value for p in ptrs]
-        self._block = _live.get(self._ptrs[0])
+    offsets (n_cols + 1, int64): first place of every column, and behind the last one the number of routed entries;
+    rows, order (nnz, int32): row and entry of R at every place; pos (nnz, int32): place of every entry.
+    Keeps R alive, whose row_ptr and val it borrows."""
 
-    def _array(self, k: int, numel: int, dtype) -> torch.Tensor:
-        if self._block is None:
-            raise GmError(-1, "Route", "its memory does not come from torch")
-        at = self._ptrs[k] - self._ptrs[0]
-        return self._block[at: at + numel * dtype.itemsize].view(dtype)
-
-    @property
-    def offsets(self) -> torch.Tensor:
-        """First place of every column, and behind the last one the number of routed entries (int64)."""
-        return self._array(0, self.n_cols + 1, torch.int64)
+    def __init__(self, handle, R: DeviceCSR, stream: int, offsets: torch.Tensor, places: torch.Tensor):
+        self._h, self.R, self._stream, self.offsets, self._places = handle, R, stream, offsets, places
+        self.n_rows, self.n_cols, self.nnz, self.device = R.n_rows, R.n_cols, R.nnz, offsets.device
 
     @property
     def rows(self) -> torch.Tensor:
-        """Row of R of the entry at every place (int32)."""
-        return self._array(1, self.nnz, torch.int32)
+        return self._places[0]
 
     @property
     def order(self) -> torch.Tensor:
-        """Entry of R at every place (int32)."""
-        return self._array(2, self.nnz, torch.int32)
+        return self._places[1]
 
     @property
     def pos(self) -> torch.Tensor:
-        """Place of every entry of R (int32)."""
-        return self._array(3, self.nnz, torch.int32)
+        return self._places[2]
 
     def status(self):
         """Raises GmError(GM_ERR_TIMEOUT) if a kernel of a finished call on this route gave up a wait."""
         _check(load_library().gm_route_status(self._h), "gm_route_status")
 
-    def _used_on(self, stream: int):
-        if stream != self._stream and self._block is not None:
+    def _current_stream(self) -> int:
+        stream = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if stream != self._stream:  # not the one its memory belongs to
             s = torch.cuda.current_stream(self.device)
-            for t in (self._block, self.R.row_ptr, self.R.val):
+            for t in (self.offsets, self._places, self.R.row_ptr, self.R.val):
                 t.record_stream(s)
+        return stream
 
     def destroy(self):
         if self._h:
@@ -451,116 +436,118 @@ class Route:
 def route_plan(R: DeviceCSR, stream=None) -> Route:
     """gm_route_plan: the entries of R (float32 values, at most 2048 columns) in the order of their columns.  An entry whose
     column is outside [0, R.n_cols) is routed nowhere."""
-    lib = load_library()
-    r = R._struct()
-    with _On("gm_route_plan", R.row_ptr.device, stream, (R.row_ptr, R.col, R.val)) as st:
-        if R.col.device != R.row_ptr.device or R.val.device != R.row_ptr.device:
-            raise GmError(-1, "gm_route_plan", "R's arrays are on different devices")
-        if R.row_ptr.numel() < R.n_rows + 1 or R.col.numel() < R.nnz or R.val.numel() < R.nnz:
-            raise GmError(-1, "gm_route_plan", "R's arrays are shorter than its sizes say")
-        h = ctypes.c_void_p()
-        _check(lib.gm_route_plan(ctypes.byref(r), st, ctypes.byref(h)), "gm_route_plan")
-        return Route(h, R, st)
-
-
-def _matrix(t: torch.Tensor, where: str, name: str, dims: int = 2):
-    if t.dim() != dims:
-        raise GmError(-2, where, f"{name}: {t.dim()} dimensions instead of {dims}")
+    where = "gm_route_plan"
+    device = R.row_ptr.device
+    if not _is_here(where, device, stream):
+        for t in (R.row_ptr, R.col, R.val):
+            if stream is not None and t.is_cuda:
+                t.record_stream(stream)
+        return _there(route_plan, device, stream, R)
+    if R.col.device != device or R.val.device != device:
+        raise GmError(-1, where, "R's arrays are on different devices")
+    if R.n_cols < 0 or R.nnz < 0 or R.row_ptr.numel() < R.n_rows + 1 or R.col.numel() < R.nnz or R.val.numel() < R.nnz:
+        raise GmError(-1, where, "R's arrays are shorter than its sizes say")
+    offsets = torch.empty(R.n_cols + 1, dtype=torch.int64, device=device)
+    places = torch.empty((3, R.nnz), dtype=torch.int32, device=device)
+    st, h, at = torch._C._cuda_getCurrentRawStream(device.index), ctypes.c_void_p(), places.data_ptr()
+    _check(load_library().gm_route_plan(_byref(R._struct()), offsets.data_ptr(), at, at + 4 * R.nnz, at + 8 * R.nnz, st, _byref(h)), where)
+    return Route(h, R, st, offsets, places)
 
 
 def route_product(route: Route, X: torch.Tensor, W: torch.Tensor, by_entry: bool = False, dtype=None, stream=None) -> torch.Tensor:
     """gm_route_product: P[p] = X[row of place p] @ W[its column].T, (nnz, N), in `dtype` (default: X's).  X (n_rows, K), or with
     by_entry (nnz, K) with a row for each place; W (n_cols, N, K); bf16 or f16."""
-    where = "gm_route_product"
-    _matrix(X, where, "X")
-    _matrix(W, where, "W", 3)
-    with _On(where, route.device, stream, (X, W)) as st:
-        P = torch.empty((route.nnz, W.shape[1]), dtype=dtype or X.dtype, device=route.device)
-        x, w, p = (_dense(t, where, route.device) for t in (X, W, P))
-        route._used_on(st)
-        _check(load_library().gm_route_product(route._h, ctypes.byref(x), int(by_entry), ctypes.byref(w), ctypes.byref(p), st), where)
-        return P
+    where, device = "gm_route_product", route.device
+    if not _is_here(where, device, stream):
+        return _there(route_product, device, stream, route, X, W, by_entry, dtype)
+    _dims(X, where, "X", 2)
+    _dims(W, where, "W", 3)
+    P = torch.empty((route.nnz, W.shape[1]), dtype=dtype or X.dtype, device=device)
+    _check(load_library().gm_route_product(route._h, _byref(_dense(X, where, device)), by_entry, _byref(_dense(W, where, device)),
+                                           _byref(_result(P)), route._current_stream()), where)
+    return P
 
 
 def route_product_dx(route: Route, dP: torch.Tensor, W: torch.Tensor, by_entry: bool = False, dtype=None, stream=None) -> torch.Tensor:
     """gm_route_product_dx: the gradient of route_product with respect to X, (n_rows, K), or (nnz, K) with by_entry."""
-    where = "gm_route_product_dx"
-    _matrix(dP, where, "dP")
-    _matrix(W, where, "W", 3)
-    with _On(where, route.device, stream, (dP, W)) as st:
-        dX = torch.empty((route.nnz if by_entry else route.n_rows, W.shape[2]), dtype=dtype or dP.dtype, device=route.device)
-        g, w, x = (_dense(t, where, route.device) for t in (dP, W, dX))
-        route._used_on(st)
-        _check(load_library().gm_route_product_dx(route._h, ctypes.byref(g), ctypes.byref(w), int(by_entry), ctypes.byref(x), st), where)
-        return dX
+    where, device = "gm_route_product_dx", route.device
+    if not _is_here(where, device, stream):
+        return _there(route_product_dx, device, stream, route, dP, W, by_entry, dtype)
+    _dims(dP, where, "dP", 2)
+    _dims(W, where, "W", 3)
+    dX = torch.empty((route.nnz if by_entry else route.n_rows, W.shape[2]), dtype=dtype or dP.dtype, device=device)
+    _check(load_library().gm_route_product_dx(route._h, _byref(_dense(dP, where, device)), _byref(_dense(W, where, device)), by_entry,
+                                              _byref(_result(dX)), route._current_stream()), where)
+    return dX
 
 
 def route_product_dw(route: Route, dP: torch.Tensor, X: torch.Tensor, by_entry: bool = False, dtype=None, stream=None) -> torch.Tensor:
     """gm_route_product_dw: the gradient of route_product with respect to W, (n_cols, N, K)."""
-    where = "gm_route_product_dw"
-    _matrix(dP, where, "dP")
-    _matrix(X, where, "X")
-    with _On(where, route.device, stream, (dP, X)) as st:
-        dW = torch.empty((route.n_cols, dP.shape[1], X.shape[1]), dtype=dtype or dP.dtype, device=route.device)
-        g, x, w = (_dense(t, where, route.device) for t in (dP, X, dW))
-        route._used_on(st)
-        _check(load_library().gm_route_product_dw(route._h, ctypes.byref(g), ctypes.byref(x), int(by_entry), ctypes.byref(w), st), where)
-        return dW
+    where, device = "gm_route_product_dw", route.device
+    if not _is_here(where, device, stream):
+        return _there(route_product_dw, device, stream, route, dP, X, by_entry, dtype)
+    _dims(dP, where, "dP", 2)
+    _dims(X, where, "X", 2)
+    dW = torch.empty((route.n_cols, dP.shape[1], X.shape[1]), dtype=dtype or dP.dtype, device=device)
+    _check(load_library().gm_route_product_dw(route._h, _byref(_dense(dP, where, device)), _byref(_dense(X, where, device)), by_entry,
+                                              _byref(_dense(dW, where, device)), route._current_stream()), where)
+    return dW
 
 
 def route_sum(route: Route, P: torch.Tensor, weighted: bool = True, dtype=None, stream=None) -> torch.Tensor:
     """gm_route_sum: Y[i] = sum over the entries of row i of R of their row of P, times R's value if `weighted`.  P (nnz, N) by place."""
-    where = "gm_route_sum"
-    _matrix(P, where, "P")
-    with _On(where, route.device, stream, (P,)) as st:
-        Y = torch.empty((route.n_rows, P.shape[1]), dtype=dtype or P.dtype, device=route.device)
-        p, y = (_dense(t, where, route.device) for t in (P, Y))
-        route._used_on(st)
-        _check(load_library().gm_route_sum(route._h, ctypes.byref(p), int(weighted), ctypes.byref(y), st), where)
-        return Y
+    where, device = "gm_route_sum", route.device
+    if not _is_here(where, device, stream):
+        return _there(route_sum, device, stream, route, P, weighted, dtype)
+    _dims(P, where, "P", 2)
+    Y = torch.empty((route.n_rows, P.shape[1]), dtype=dtype or P.dtype, device=device)
+    _check(load_library().gm_route_sum(route._h, _byref(_dense(P, where, device)), weighted, _byref(_result(Y)), route._current_stream()), where)
+    return Y
 
 
 def route_sum_grads(route: Route, dY: torch.Tensor, P: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
     """gm_route_sum_grads: gradients of the weighted route_sum, dP (nnz, N) by place and dval (nnz,) float32 by entry of R."""
-    where = "gm_route_sum_grads"
-    _matrix(dY, where, "dY")
-    _matrix(P, where, "P")
-    with _On(where, route.device, stream, (dY, P)) as st:
-        dP = torch.empty((route.nnz, P.shape[1]), dtype=P.dtype, device=route.device)
-        dval = torch.empty(route.nnz, dtype=torch.float32, device=route.device)
-        g, p, d = (_dense(t, where, route.device) for t in (dY, P, dP))
-        route._used_on(st)
-        _check(load_library().gm_route_sum_grads(route._h, ctypes.byref(g), ctypes.byref(p), ctypes.byref(d), dval.data_ptr(), st), where)
-        return dP, dval
+    where, device = "gm_route_sum_grads", route.device
+    if not _is_here(where, device, stream):
+        return _there(route_sum_grads, device, stream, route, dY, P)
+    _dims(dY, where, "dY", 2)
+    _dims(P, where, "P", 2)
+    dP = torch.empty((route.nnz, P.shape[1]), dtype=P.dtype, device=device)
+    dval = torch.empty(route.nnz, dtype=torch.float32, device=device)
+    _check(load_library().gm_route_sum_grads(route._h, _byref(_dense(dY, where, device)), _byref(_dense(P, where, device)), _byref(_result(dP)),
+                                             dval.data_ptr(), route._current_stream()), where)
+    return dP, dval
 
 
 def block_quantize(X: torch.Tensor, block_rows: int = 1, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
     """gm_block_quantize: (values in float8_e4m3fn, float32 scales) of X (rows, K) or (blocks, rows, K), bf16 or f16, with a scale for
     each block of block_rows (1 or 128) x 128."""
-    where = "gm_block_quantize"
-    if X.dim() not in (2, 3):
-        raise GmError(-2, where, f"X: {X.dim()} dimensions instead of 2 or 3")
+    where, device = "gm_block_quantize", X.device
+    if not _is_here(where, device, stream):
+        return _there(block_quantize, device, stream, X, block_rows)
     if block_rows not in (1, 128):
         raise GmError(-1, where, "block_rows: 1 or 128 expected")
-    with _On(where, X.device, stream, (X,)) as st:
-        Q = torch.empty(X.shape, dtype=torch.float8_e4m3fn, device=X.device)
-        S = torch.empty((*X.shape[:-2], -(-X.shape[-2] // block_rows), -(-X.shape[-1] // 128)), dtype=torch.float32, device=X.device)
-        x, q, s = (_dense(t, where, X.device) for t in (X, Q, S))
-        _check(load_library().gm_block_quantize(ctypes.byref(x), block_rows, ctypes.byref(q), ctypes.byref(s), st), where)
-        return Q, S
+    shape = X.shape
+    if len(shape) not in (2, 3):
+        raise GmError(-2, where, f"X: {len(shape)} dimensions instead of 2 or 3")
+    Q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
+    S = torch.empty((*shape[:-2], -(-shape[-2] // block_rows), -(-shape[-1] // 128)), dtype=torch.float32, device=device)
+    _check(load_library().gm_block_quantize(_byref(_dense(X, where, device)), block_rows, _byref(_dense(Q, where, device)),
+                                            _byref(_dense(S, where, device)), torch._C._cuda_getCurrentRawStream(device.index)), where)
+    return Q, S
 
 
 def route_product_scaled(route: Route, Xq: torch.Tensor, Xs: torch.Tensor, Wq: torch.Tensor, Ws: torch.Tensor, by_entry: bool = False,
-                       dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+                         dtype=torch.bfloat16, stream=None) -> torch.Tensor:
     """gm_route_product_scaled: route_product of float8_e4m3fn factors with scales, as block_quantize gives them: Xs (rows of X, K / 128),
     Ws (n_cols, N / 128, K / 128) or (n_cols, N, K / 128), all rounded up."""
-    where = "gm_route_product_scaled"
+    where, device = "gm_route_product_scaled", route.device
+    if not _is_here(where, device, stream):
+        return _there(route_product_scaled, device, stream, route, Xq, Xs, Wq, Ws, by_entry, dtype)
     for t, name, dims in ((Xq, "Xq", 2), (Xs, "Xs", 2), (Wq, "Wq", 3), (Ws, "Ws", 3)):
-        _matrix(t, where, name, dims)
-    with _On(where, route.device, stream, (Xq, Xs, Wq, Ws)) as st:
-        P = torch.empty((route.nnz, Wq.shape[1]), dtype=dtype, device=route.device)
-        xq, xs, wq, ws, p = (_dense(t, where, route.device) for t in (Xq, Xs, Wq, Ws, P))
-        route._used_on(st)
-        _check(load_library().gm_route_product_scaled(route._h, ctypes.byref(xq), ctypes.byref(xs), int(by_entry), ctypes.byref(wq),
-                                                    ctypes.byref(ws), ctypes.byref(p), st), where)
-        return P
+        _dims(t, where, name, dims)
+    P = torch.empty((route.nnz, Wq.shape[1]), dtype=dtype, device=device)
+    _check(load_library().gm_route_product_scaled(route._h, _byref(_dense(Xq, where, device)), _byref(_dense(Xs, where, device)), by_entry,
+                                                  _byref(_dense(Wq, where, device)), _byref(_dense(Ws, where, device)), _byref(_result(P)),
+                                                  route._current_stream()), where)
+    return P

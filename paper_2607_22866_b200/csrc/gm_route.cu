@@ -3,6 +3,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 #include <new>
 
@@ -19,13 +20,11 @@ struct gm_route {
   int E = 0;
   const i64* row_ptr = nullptr;
   const float* val = nullptr;
-  void* block = nullptr;  // offsets, rows, order, pos
   i64* offsets = nullptr;
   int32_t* rows = nullptr;
   int32_t* order = nullptr;
   int32_t* pos = nullptr;
   int* err = nullptr;     // page-locked: the first problem of a kernel
-  cudaStream_t stream = nullptr;
 };
 
 namespace gm {
@@ -170,8 +169,18 @@ static int route_ready(const gm_route* r) {
   return GM_OK;
 }
 
-static int set_smem(const void* kernel, size_t bytes) {
-  GM_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+// The most dynamic shared memory these kernels ask for (what a block may have, less their static arrays), allowed once per device.
+constexpr int kMostSmem = 232448 - 1024;
+struct SmemAllowed { std::atomic<unsigned long long> devices{0}; };
+template <auto kernel>
+static int allow_most_smem() {
+  static SmemAllowed allowed;
+  int dev = 0;
+  GM_CUDA(cudaGetDevice(&dev));
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (allowed.devices.load(std::memory_order_relaxed) & bit) return GM_OK;
+  GM_CUDA(cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
+  allowed.devices.fetch_or(bit, std::memory_order_relaxed);
   return GM_OK;
 }
 
@@ -179,7 +188,7 @@ constexpr size_t kT5Smem = static_cast<size_t>(kStages) * kStage + 1024 + sizeof
 static size_t product_smem(int E, bool bits8) {
   return kT5Smem + static_cast<size_t>(E + 1) * 8 + (bits8 ? 16 + 2 * 4 * kTileN * 4 : 0);
 }
-static_assert(kT5Smem + (kRouteMaxCols + 1) * 8 + 16 + 2 * 4 * kTileN * 4 <= 232448, "fits a block's shared memory");
+static_assert(kT5Smem + (kRouteMaxCols + 1) * 8 + 16 + 2 * 4 * kTileN * 4 <= kMostSmem, "fits a block's shared memory");
 
 // A result of no terms: rows of zeros.
 static int zero_out(const gm_dense& M, cudaStream_t st) {
@@ -191,9 +200,9 @@ static int zero_out(const gm_dense& M, cudaStream_t st) {
 }
 
 // A pair of blocks per tile, at most one pair per two SMs.
-template <typename... A>
-static int launch_t5(void (*kernel)(A...), i64 tiles, int num_sms, int threads, size_t smem, cudaStream_t st, const A&... args) {
-  GM_TRY(set_smem(reinterpret_cast<const void*>(kernel), smem));
+template <auto kernel, typename... A>
+static int launch_t5(i64 tiles, int num_sms, int threads, size_t smem, cudaStream_t st, const A&... args) {
+  GM_TRY(allow_most_smem<kernel>());
   kernel<<<static_cast<unsigned>(2 * std::max<i64>(1, std::min<i64>(tiles, num_sms / 2))), threads, smem, st>>>(args...);
   GM_CUDA(cudaGetLastError());
   return GM_OK;
@@ -257,11 +266,11 @@ static int product(const gm_route* r, const gm_dense& X, bool by_entry, const gm
   a.err = r->err;
   const i64 tiles = ((r->nnz + kTileN - 1) / kTileN + std::min<i64>(r->E, r->nnz)) * ((n_m + kTileM - 1) / kTileM);
   const size_t smem = product_smem(r->E, false);
-  const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, by_entry ? 192 : 352, smem, st, map_w, map_x, a); };
+  const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, by_entry ? 192 : 352, smem, st, map_w, map_x, a); };
   const auto typed = [&](auto* tag) {
     using TO = std::remove_pointer_t<decltype(tag)>;
-    if (m_inner) return by_entry ? go(k_route_product<true, false, TO>) : go(k_route_product<true, true, TO>);
-    return by_entry ? go(k_route_product<false, false, TO>) : go(k_route_product<false, true, TO>);
+    if (m_inner) return by_entry ? go.template operator()<k_route_product<true, false, TO>>() : go.template operator()<k_route_product<true, true, TO>>();
+    return by_entry ? go.template operator()<k_route_product<false, false, TO>>() : go.template operator()<k_route_product<false, true, TO>>();
   };
   switch (out.dtype) {
     case GM_F32: return typed(static_cast<float*>(nullptr));
@@ -345,7 +354,7 @@ using namespace gm;
 
 extern "C" {
 
-int gm_route_plan(const gm_csr* R, void* cuda_stream, gm_route** route_out) {
+int gm_route_plan(const gm_csr* R, int64_t* offsets, int32_t* rows, int32_t* order, int32_t* pos, void* cuda_stream, gm_route** route_out) {
   return guarded([&]() -> int {
     if (!R || !route_out) return fail(GM_ERR_INVALID_ARG, "null argument");
     *route_out = nullptr;
@@ -354,6 +363,7 @@ int gm_route_plan(const gm_csr* R, void* cuda_stream, gm_route** route_out) {
     if (R->n_cols > kRouteMaxCols) return fail(GM_ERR_CAPACITY, "R: more than " + std::to_string(kRouteMaxCols) + " columns");
     if (R->n_rows == 0 && R->nnz > 0) return fail(GM_ERR_BAD_CSR, "R: entries without rows");
     if (!R->row_ptr || (R->nnz > 0 && (!R->col_idx || !R->vals))) return fail(GM_ERR_INVALID_ARG, "R: null array");
+    if (!offsets || (R->nnz > 0 && (!rows || !order || !pos))) return fail(GM_ERR_INVALID_ARG, "null array");
     if (R->dtype != GM_F32) return fail(GM_ERR_DTYPE, "R: f32 values expected");
     int num_sms, smem_optin;
     GM_TRY(device_facts_basic(&num_sms, &smem_optin));
@@ -366,17 +376,12 @@ int gm_route_plan(const gm_csr* R, void* cuda_stream, gm_route** route_out) {
     r->E = static_cast<int>(R->n_cols);
     r->row_ptr = R->row_ptr;
     r->val = static_cast<const float*>(R->vals);
-    r->stream = st;
     r->err = take_error_word();
     if (!r->err) return drop(fail(GM_ERR_OOM, "no page-locked memory"));
-    const size_t n_off = (static_cast<size_t>(r->E + 1) * 8 + 15) / 16 * 16, n_arr = (static_cast<size_t>(r->nnz) * 4 + 15) / 16 * 16;
-    r->block = dev_alloc(n_off + 3 * n_arr, st);
-    if (!r->block) return drop(fail(GM_ERR_OOM, "no room for the route"));
-    char* p = static_cast<char*>(r->block);
-    r->offsets = reinterpret_cast<i64*>(p);
-    r->rows = reinterpret_cast<int32_t*>(p + n_off);
-    r->order = reinterpret_cast<int32_t*>(p + n_off + n_arr);
-    r->pos = reinterpret_cast<int32_t*>(p + n_off + 2 * n_arr);
+    r->offsets = offsets;
+    r->rows = rows;
+    r->order = order;
+    r->pos = pos;
     // one block up to 4096 entries (four per thread), then as many as give every thread that many
     const int warps = route_warps(r->E);
     unsigned blocks = 1;
@@ -393,7 +398,7 @@ int gm_route_plan(const gm_csr* R, void* cuda_stream, gm_route** route_out) {
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    int rc = set_smem(reinterpret_cast<const void*>(k_route_plan), smem);
+    int rc = allow_most_smem<k_route_plan>();
     if (rc != GM_OK) return drop(rc);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, k_route_plan, r->row_ptr, R->col_idx, static_cast<int>(r->n_rows), r->nnz, r->E,
                                              r->offsets, r->rows, r->order, r->pos);
@@ -403,20 +408,10 @@ int gm_route_plan(const gm_csr* R, void* cuda_stream, gm_route** route_out) {
   });
 }
 
-int gm_route_arrays(const gm_route* route, const int64_t** offsets, const int32_t** rows, const int32_t** order, const int32_t** pos) {
-  if (!route || !offsets || !rows || !order || !pos) return fail(GM_ERR_INVALID_ARG, "null argument");
-  *offsets = route->offsets;
-  *rows = route->rows;
-  *order = route->order;
-  *pos = route->pos;
-  return GM_OK;
-}
-
 int gm_route_status(const gm_route* route) { return guarded([&]() -> int { return route_ready(route); }); }
 
 void gm_route_destroy(gm_route* route) {
   if (!route) return;
-  if (route->block) dev_free(route->block, route->stream);
   give_error_word(route->err);
   delete route;
 }
@@ -503,11 +498,11 @@ int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dens
     a.type = dP->dtype == GM_BF16 ? 1 : 0;
     a.err = route->err;
     const i64 tiles = static_cast<i64>(a.E) * ((a.n_m + kTileM - 1) / kTileM) * ((a.n_j + kTileN - 1) / kTileN);
-    const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, 320, kT5Smem, st, a); };
+    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 320, kT5Smem, st, a); };
     switch (dW->dtype) {
-      case GM_F32: return by_entry ? go(k_route_dw<false, float>) : go(k_route_dw<true, float>);
-      case GM_BF16: return by_entry ? go(k_route_dw<false, __nv_bfloat16>) : go(k_route_dw<true, __nv_bfloat16>);
-      default: return by_entry ? go(k_route_dw<false, __half>) : go(k_route_dw<true, __half>);
+      case GM_F32: return by_entry ? go.template operator()<k_route_dw<false, float>>() : go.template operator()<k_route_dw<true, float>>();
+      case GM_BF16: return by_entry ? go.template operator()<k_route_dw<false, __nv_bfloat16>>() : go.template operator()<k_route_dw<true, __nv_bfloat16>>();
+      default: return by_entry ? go.template operator()<k_route_dw<false, __half>>() : go.template operator()<k_route_dw<true, __half>>();
     }
   });
 }
@@ -679,11 +674,11 @@ int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_
     a.err = route->err;
     const i64 tiles = ((route->nnz + kTileN - 1) / kTileN + std::min<i64>(route->E, route->nnz)) * ((a.n_m + kTileM - 1) / kTileM);
     const size_t smem = product_smem(route->E, true);
-    const auto go = [&](auto kernel) { return launch_t5(kernel, tiles, num_sms, by_entry ? 384 : 512, smem, st, map_w, map_x, a); };
+    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, by_entry ? 384 : 512, smem, st, map_w, map_x, a); };
     const auto typed = [&](auto* tag) {
       using TO = std::remove_pointer_t<decltype(tag)>;
-      if (row_scales) return by_entry ? go(k_route_product_scaled<false, true, TO>) : go(k_route_product_scaled<true, true, TO>);
-      return by_entry ? go(k_route_product_scaled<false, false, TO>) : go(k_route_product_scaled<true, false, TO>);
+      if (row_scales) return by_entry ? go.template operator()<k_route_product_scaled<false, true, TO>>() : go.template operator()<k_route_product_scaled<true, true, TO>>();
+      return by_entry ? go.template operator()<k_route_product_scaled<false, false, TO>>() : go.template operator()<k_route_product_scaled<true, false, TO>>();
     };
     switch (P->dtype) {
       case GM_F32: return typed(static_cast<float*>(nullptr));
