@@ -382,27 +382,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
 }
 
 // 8 bits.  The sums of 128 values of k go to a buffer of their own in tensor memory; eight warps take them out, multiply by both
-// scales and add them up in registers (a thread: one row of W, half the places of the tile).
-// kRowScales: W has scales for each row and 128 values; else for each 128 rows, so that a block's half of the tile has one.
-// Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 4-11 results.  The results' registers are what the others
-// give up: 512 threads begin with 128 each (384 with 168).
+// scales and add them up in registers (a thread: one row of W, half the places of the tile).  The scales come through a ring in
+// shared memory, a slot per block of k: those of the tile's places, times W's where it has one for each 128 rows, or 128 of W's behind
+// them (kRowScales).
+// Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 3 scales, 4-11 results.  The results' registers
+// are what the others give up: 512 threads begin with 128 each (384 with 168).
+constexpr int kScaleSlots = 8;
+constexpr int kScaleLag = 4;               // slots whose copies may be under way
+constexpr int kScaleSlot = kTileN + 128;  // floats
+struct ScaleBlock { u64 full[kScaleSlots], empty[kScaleSlots]; };
+
 template <bool kGather, bool kRowScales, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384, 1)
     k_route_product_scaled(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const ProductArgs a) {
-  constexpr int kAhead = 4;  // blocks of k whose scales are brought in together
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
-  T5Block* b = reinterpret_cast<T5Block*>(stages + kStages * kStage);
-  float* scale = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(b + 1) + 15) & ~static_cast<uintptr_t>(15));  // [2][kAhead][kTileN]
-  int* off = reinterpret_cast<int*>(scale + 2 * kAhead * kTileN);
+  float* scales = reinterpret_cast<float*>(stages + kStages * kStage);
+  T5Block* b = reinterpret_cast<T5Block*>(scales + kScaleSlots * kScaleSlot);
+  ScaleBlock* sb = reinterpret_cast<ScaleBlock*>(b + 1);
+  int* off = reinterpret_cast<int*>(sb + 1);
   int* part = off + a.E + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const u32 rank = cluster_rank();
+  if (threadIdx.x == 32)
+    for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&sb->full[i], 1); mbar_init(&sb->empty[i], 8); }
   t5_begin(b, kGather ? 3 : 1, 8);
   list_parts(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 127) / 128;
   const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
-  const u32 stage0 = smem_u32(stages), tmem = b->tmem;
+  const u32 stage0 = smem_u32(stages), scale0 = smem_u32(scales), tmem = b->tmem;
   zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
 
   if (warp < 4) {
@@ -416,12 +424,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
         const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
         const u32 idesc = t5_idesc(a.type, false, false, kTileM, round32(t.n));
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
-          const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kHalf, buf = it & 1, d = tmem + buf * kTileN;
+          const u32 s = it % kStages, sa = stage0 + s * kStage, sx = sa + kHalf, buf = it & 1, d = tmem + buf * kTileN;
           ok = t5_wait(&b->sums_empty[buf], ((it >> 1) & 1) ^ 1) && t5_wait(&b->full[s], (it / kStages) & 1);
           if (!ok) break;
           t5_fence_after();
 #pragma unroll
-          for (int j = 0; j < 4; ++j) t5_mma_f8(d, t5_desc_k(sa + j * 32), t5_desc_k(sb + j * 32), idesc, j > 0);
+          for (int j = 0; j < 4; ++j) t5_mma_f8(d, t5_desc_k(sa + j * 32), t5_desc_k(sx + j * 32), idesc, j > 0);
           t5_commit(&b->empty[s]);
           t5_commit(&b->sums_full[buf]);
         }
@@ -430,89 +438,118 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
         dev_set_error(a.err, kDevTimeout);
         t5_drain_matrix(b);
       }
+    } else if (kGather && warp == 2 && lane == 0) {
+      hand_over_rows(a, b, n_tiles, n_kb);
+    } else if (warp == 3) {
+      u32 it = 0;
+      bool ok = true;
+      const auto hand_scales = [&](u32 i) {  // a slot whose copies have arrived: each lane multiplies what it has copied itself
+        float* at = scales + i % kScaleSlots * kScaleSlot + lane;
+        if (!kRowScales) {
+          const float w = at[kTileN];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) at[32 * j] *= w;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sb->full[i % kScaleSlots]);
+      };
+      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+        const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+        const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128;
+        const float* ws = a.ws + static_cast<i64>(t.e) * a.ws_block;
+        int row[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int p = lane + 32 * i;
+          row[i] = p < t.n ? (kGather ? a.rows[t.first + p] : t.first + p) : -1;
+        }
+        for (int kb = 0; kb < n_kb; ++kb, ++it) {
+          const u32 s = it % kScaleSlots, to = scale0 + (s * kScaleSlot + lane) * 4;
+          ok = __all_sync(0xffffffffu, t5_wait(&sb->empty[s], ((it / kScaleSlots) & 1) ^ 1));
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (row[i] >= 0) copy4(to + 128 * i, a.xs + row[i] * a.xs_stride + kb);
+          if (kRowScales) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (m0 + lane + 32 * i < a.n_m) copy4(to + (kTileN + 32 * i) * 4, ws + static_cast<i64>(m0 + lane + 32 * i) * a.ws_row + kb);
+          } else {  // (every lane has its own copy of W's)
+            copy4(to + kTileN * 4, ws + static_cast<i64>(min(m0, a.n_m - 1) / 128) * a.ws_row + kb);
+          }
+          copy_commit();
+          if (it >= kScaleLag) {
+            copy_wait<kScaleLag>();
+            hand_scales(it - kScaleLag);
+          }
+        }
+      }
+      copy_wait_all();
+      for (u32 i = it > kScaleLag ? it - kScaleLag : 0; i < it; ++i) hand_scales(i);
+      if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
     }
-    if (kGather && warp == 2 && lane == 0) hand_over_rows(a, b, n_tiles, n_kb);
     __syncwarp();
   } else if (warp < 12) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(208));
-    const int quad = warp & 3, half = (warp - 4) >> 2, tid = threadIdx.x - 128;
+    const int quad = warp & 3, half = (warp - 4) >> 2;
     u32 it = 0;
     bool ok = true;
-    // (a wait that gave up skips the work from there on, not the barriers among these warps)
-    for (i64 id = blockIdx.x >> 1; id < n_tiles; id += gridDim.x >> 1) {
+    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
       const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128, m = m0 + quad * 32 + lane;
-      float acc[4][32];
+      const int m = static_cast<int>(id % n_mt) * kTileM + rank * 128 + quad * 32 + lane;
+      const int mine = t.n - half * 128;  // places of this warp's half of the columns
+      u64 acc[64];                        // two places each
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int j = 0; j < 32; ++j) acc[c][j] = 0.f;
-      // this thread brings in the scales of place `tid` of the tile
-      const float* xs = nullptr;
-      if (tid < t.n) xs = a.xs + static_cast<i64>(kGather ? a.rows[t.first + tid] : t.first + tid) * a.xs_stride;
-      const float* ws = a.ws + static_cast<i64>(t.e) * a.ws_block +
-                        (kRowScales ? static_cast<i64>(min(m, a.n_m - 1)) : static_cast<i64>(min(m0, a.n_m - 1) / 128)) * a.ws_row;
-      float next[kAhead], wnext[kAhead];
-      auto fetch = [&](int kb) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          wnext[i] = kb + i < n_kb ? ws[kb + i] : 0.f;
-          next[i] = xs && kb + i < n_kb ? xs[kb + i] : 0.f;
+      for (int j = 0; j < 64; ++j) acc[j] = 0;
+#pragma unroll 1
+      for (int kb = 0; kb < n_kb; ++kb, ++it) {
+        const u32 buf = it & 1, s = it % kScaleSlots;
+        ok = __all_sync(0xffffffffu, t5_wait(&sb->full[s], (it / kScaleSlots) & 1) && t5_wait(&b->sums_full[buf], (it >> 1) & 1));
+        if (!ok) break;
+        t5_fence_after();
+        const u32 from = tmem + buf * kTileN + half * 128 + (static_cast<u32>(quad * 32) << 16);
+        const float4* sx = reinterpret_cast<const float4*>(scales + s * kScaleSlot + half * 128);
+        u64 w2 = 0;
+        if (kRowScales) {
+          const u32 w = __float_as_uint(scales[s * kScaleSlot + kTileN + quad * 32 + lane]);
+          w2 = pair_of(w, w);
         }
-      };
-      fetch(0);
-      for (int kb0 = 0; kb0 < n_kb; kb0 += kAhead) {
-        float* sc = scale + ((kb0 / kAhead) & 1) * kAhead * kTileN;
-        float w[kAhead];
+        u32 v[2][16];
+        t5_ld16(v[0], from);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          w[i] = wnext[i];
-          sc[i * kTileN + tid] = kRowScales ? next[i] : next[i] * wnext[i];
-        }
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        if (kb0 + kAhead < n_kb) fetch(kb0 + kAhead);
+        for (int c = 0; c < 8; ++c) {  // sixteen places: the next ones are on their way while these are added up
+          if (c * 16 < mine || c == 0) {
+            u64 x[8];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          if (kb0 + i < n_kb && ok) {
-            const u32 buf = it & 1;
-            ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (it >> 1) & 1));
-            if (ok) {
-              t5_fence_after();
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                if (half * 128 + c * 32 < t.n) {
-                  u32 v[32];
-                  t5_ld32(v, tmem + buf * kTileN + half * 128 + c * 32 + (static_cast<u32>(quad * 32) << 16));
-                  t5_wait_ld();
-                  const float4* s4 = reinterpret_cast<const float4*>(sc + i * kTileN + half * 128 + c * 32);
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) {
-                    const float4 s = s4[j];
-                    acc[c][4 * j + 0] += __uint_as_float(v[4 * j + 0]) * (kRowScales ? s.x * w[i] : s.x);
-                    acc[c][4 * j + 1] += __uint_as_float(v[4 * j + 1]) * (kRowScales ? s.y * w[i] : s.y);
-                    acc[c][4 * j + 2] += __uint_as_float(v[4 * j + 2]) * (kRowScales ? s.z * w[i] : s.z);
-                    acc[c][4 * j + 3] += __uint_as_float(v[4 * j + 3]) * (kRowScales ? s.w * w[i] : s.w);
-                  }
-                }
-              }
+            for (int j = 0; j < 4; ++j) {
+              const float4 f = sx[c * 4 + j];
+              x[2 * j] = pair_of(__float_as_uint(f.x), __float_as_uint(f.y));
+              x[2 * j + 1] = pair_of(__float_as_uint(f.z), __float_as_uint(f.w));
+            }
+            t5_wait_ld16(v[c & 1]);
+            if (c + 1 < 8 && (c + 1) * 16 < mine) {
+              t5_ld16(v[(c + 1) & 1], from + (c + 1) * 16);
+            } else {  // all out: the buffer is free
               t5_fence_before();
               if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
-              ++it;
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              fma2(acc[c * 8 + j], pair_of(v[c & 1][2 * j], v[c & 1][2 * j + 1]), kRowScales ? mul2(x[j], w2) : x[j]);
           }
         }
+        if (lane == 0) mbar_arrive(&sb->empty[s]);
       }
       if (ok) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const int at = half * 128 + c * 32;
           u32 v[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(acc[c][j]);
-          if (at < t.n) store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + at, t.n - at, m, a.n_m, v);
+          for (int j = 0; j < 16; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(v[2 * j]), "=r"(v[2 * j + 1]) : "l"(acc[c * 16 + j]));
+          if (c * 32 < mine)
+            store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + half * 128 + c * 32, mine - c * 32, m, a.n_m, v);
         }
       }
-      asm volatile("bar.sync 1, 256;" ::: "memory");  // (the scales' buffers go round again)
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   } else {

@@ -185,10 +185,11 @@ static int allow_most_smem() {
 }
 
 constexpr size_t kT5Smem = static_cast<size_t>(kStages) * kStage + 1024 + sizeof(T5Block);
+constexpr size_t kScaleSmem = kScaleSlots * kScaleSlot * 4 + sizeof(ScaleBlock);
 static size_t product_smem(int E, bool bits8) {
-  return kT5Smem + static_cast<size_t>(E + 1) * 8 + (bits8 ? 16 + 2 * 4 * kTileN * 4 : 0);
+  return kT5Smem + static_cast<size_t>(E + 1) * 8 + (bits8 ? kScaleSmem : 0);
 }
-static_assert(kT5Smem + (kRouteMaxCols + 1) * 8 + 16 + 2 * 4 * kTileN * 4 <= kMostSmem, "fits a block's shared memory");
+static_assert(kT5Smem + (kRouteMaxCols + 1) * 8 + kScaleSmem <= kMostSmem, "fits a block's shared memory");
 
 // A result of no terms: rows of zeros.
 static int zero_out(const gm_dense& M, cudaStream_t st) {
