@@ -559,17 +559,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
   t5_end(tmem);
 }
 
-// Both operands lie with the reduction (64 places a stage) across their rows and come by index, 16 bytes at a time: what lies behind a
-// column's last place is not read but zero, so that a sum ends inside a stage whatever its neighbour holds.
-// Warps: 0 hands over what 6-9 copy, 1 matrix instructions, 2-5 results.
+// Both operands lie with the reduction (64 places a stage) across their rows.  Stages of 64 places of one column come by tensor map (dP, and X
+// with a row per place); rows by index, and a column's last places, 16 bytes at a time by four warps: what lies behind the last place is
+// not read but zero, so that a sum ends inside a stage whatever its neighbour holds.
+// Warps: 0 copies by tensor map, 1 matrix instructions, 2-5 results, 6-9 copies, 10 hands those over.
 template <bool kGather, typename TO>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(320, 1) k_route_dw(const DwArgs a) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
+    k_route_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const DwArgs a) {
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
   T5Block* b = reinterpret_cast<T5Block*>(stages + kStages * kStage);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const u32 rank = cluster_rank();
-  t5_begin(b, 2, 4);
+  t5_begin(b, 3, 4);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_jt = (a.n_j + kTileN - 1) / kTileN, n_per = n_mt * n_jt;
   const i64 n_tiles = static_cast<i64>(a.E) * n_per;
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
@@ -580,11 +582,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(320, 1) k_route_dw(c
       u32 it = 0;
       bool ok = true;
       for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-        const int e = static_cast<int>(id / n_per), n_st = (static_cast<int>(a.offsets[e + 1] - a.offsets[e]) + 63) / 64;
-        for (int i = 0; ok && i < n_st; ++i, ++it) ok = hand_over(b, it);
+        const int e = static_cast<int>(id / n_per), rest = static_cast<int>(id % n_per);
+        const int j0 = rest / n_mt * kTileN, half = a.n_j - j0 > 128 ? 128 : 64;
+        const int m = rest % n_mt * kTileM + rank * 128, j = j0 + rank * half;
+        const int p0 = static_cast<int>(a.offsets[e]), p1 = static_cast<int>(a.offsets[e + 1]);
+        for (int p = p0; p < p1; p += 64, ++it) {
+          const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kHalf;
+          ok = t5_wait(&b->empty[s], ((it / kStages) & 1) ^ 1);
+          if (!ok) break;
+          const bool whole = p + 64 <= p1;
+          if (rank == 0) mbar_arrive_expect_tx(&b->full[s], whole ? 2 * (2 + (kGather ? 0 : half / 64)) * kBlock : 0);
+          if (whole) {
+            const u32 bar = leader_bar(&b->full[s]);
+            tma_load_2d(sa, &map_p, m, p, bar);
+            tma_load_2d(sa + kBlock, &map_p, m + 64, p, bar);
+            if (!kGather) {
+              tma_load_2d(sb, &map_x, j, p, bar);
+              if (half > 64) tma_load_2d(sb + kBlock, &map_x, j + 64, p, bar);
+            }
+          }
+        }
       }
-      if (!ok) dev_set_error(a.err, kDevTimeout);
+      if (!ok) {
+        dev_set_error(a.err, kDevTimeout);
+        if (rank == 0) t5_drain_copies(b, it);
+      }
     }
+    __syncwarp();
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       u32 it = 0, n_done = 0;
@@ -616,6 +640,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(320, 1) k_route_dw(c
       }
     }
     __syncwarp();
+  } else if (warp == 10) {
+    if (lane == 0) {
+      u32 it = 0;
+      bool ok = true;
+      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+        const int e = static_cast<int>(id / n_per), n_st = (static_cast<int>(a.offsets[e + 1] - a.offsets[e]) + 63) / 64;
+        for (int i = 0; ok && i < n_st; ++i, ++it) ok = hand_over(b, it);
+      }
+      if (!ok) dev_set_error(a.err, kDevTimeout);
+    }
+    __syncwarp();
   } else if (warp >= 6) {
     // sixteen lanes have a row: 256 bytes of dP, 256 (or 128) of X
     const int thread = threadIdx.x - 192, c = thread & 15, r0 = thread >> 4;
@@ -630,31 +665,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(320, 1) k_route_dw(c
       const u32 m_bytes = 2 * max(0, min(8, a.n_m - m)), j_bytes = 2 * max(0, min(8, a.n_j - j));
       const char* dp = a.dp + (m_bytes ? 2 * static_cast<i64>(m) : 0);
       const char* x = a.x + (j_bytes ? 2 * static_cast<i64>(j) : 0);
-      int next[8];
+      int next[8], after[8];  // rows of X of the next stage and the one behind it
+      const auto rows_at = [&](int p, int (&to)[8]) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int q = p0 + r0 + 8 * i;
-        next[i] = q < p1 ? (kGather ? a.rows[q] : q) : -1;
-      }
+        for (int i = 0; i < 8; ++i) {
+          const int q = p + r0 + 8 * i;
+          to[i] = q < p1 ? (kGather ? a.rows[q] : q) : -1;
+        }
+      };
+      rows_at(p0, next);
+      rows_at(p0 + 64, after);
       for (int p = p0; p < p1; p += 64) {
         ok = queue.slot_free();
         if (!ok) break;
         const u32 dst = stage0 + queue.issued % kStages * kStage + at;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int q = p + r0 + 8 * i;
-          copy16(dst + i * 8 * kRowBytes, q < p1 ? dp + q * a.dp_stride : dp, q < p1 ? m_bytes : 0);
-        }
-        if (c * 8 < half) {
+        const bool whole = p + 64 <= p1;
+        if ((kGather || !whole) && c * 8 < half) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             copy16(dst + kHalf + i * 8 * kRowBytes, next[i] >= 0 ? x + next[i] * a.x_stride : x, next[i] >= 0 ? j_bytes : 0);
         }
+        if (!whole) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int q = p + 64 + r0 + 8 * i;
-          next[i] = q < p1 ? (kGather ? a.rows[q] : q) : -1;
+          for (int i = 0; i < 8; ++i) {
+            const int q = p + r0 + 8 * i;
+            copy16(dst + i * 8 * kRowBytes, q < p1 ? dp + q * a.dp_stride : dp, q < p1 ? m_bytes : 0);
+          }
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) next[i] = after[i];
+        rows_at(p + 128, after);
         queue.done();
       }
     }

@@ -77,16 +77,30 @@ template <typename T, bool kVec> struct Raw {
   static __device__ __forceinline__ type load(const T* p) { return *p; }
   static __device__ __forceinline__ void values(const type& r, float (&v)[8]) { v[0] = static_cast<float>(r); }
 };
-template <typename T> struct Raw<T, true> {
-  struct alignas(16) type { T v[8]; };
+template <typename T> struct Raw<T, true> {  // 16 bytes
+  struct alignas(16) type { T v[16 / sizeof(T)]; };
   static __device__ __forceinline__ type load(const T* p) {
     type r;
-#pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(type) / 16); ++i) reinterpret_cast<uint4*>(&r)[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    *reinterpret_cast<uint4*>(&r) = __ldcs(reinterpret_cast<const uint4*>(p));
     return r;
   }
-  static __device__ __forceinline__ void values(const type& r, float (&v)[8]) { Vec8<T>::load(r.v, v); }
+  static __device__ __forceinline__ void values(const type& r, float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = r.v[i];
+    } else {
+      Vec8<T>::load(r.v, v);
+    }
+  }
 };
+template <typename T> __device__ __forceinline__ void store4(T* p, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    struct alignas(8) { T t[4]; } w = {{from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])}};
+    *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(&w);
+  }
+}
 
 struct SumArgs {
   const i64* row_ptr;
@@ -106,39 +120,51 @@ struct SumArgs {
 
 constexpr int kSumThreads = 128;
 
-template <typename TI, typename TO, bool kVec>
+// kUnits: runs of columns per thread, kSumThreads runs apart; eight loads are in flight, for 8 / kUnits entries.
+template <typename TI, typename TO, bool kVec, int kUnits>
 __global__ void __launch_bounds__(kSumThreads) k_route_sum(const SumArgs a, int n_chunks) {
-  constexpr int kCols = kVec ? 8 : 1;
+  constexpr int kCols = kVec ? 16 / sizeof(TI) : 1, kEntries = 8 / kUnits, kStep = kSumThreads * kCols;
   const i64 i = blockIdx.x / n_chunks;
-  const int c = (static_cast<int>(blockIdx.x % n_chunks) * kSumThreads + threadIdx.x) * kCols;
+  const int c = static_cast<int>(blockIdx.x % n_chunks) * kUnits * kStep + threadIdx.x * kCols;
   if (c >= a.width) return;
   const i64 q0 = max(static_cast<i64>(0), a.row_ptr[i]), q1 = min(a.entries, a.row_ptr[i + 1]);
   const int routed = static_cast<int>(a.offsets[a.E]);
   const TI* p = static_cast<const TI*>(a.p) + c;
-  float acc[8] = {};
-  for (i64 q = q0; q < q1; q += 8) {  // eight rows in flight: their places first, then their values, then the sums
-    int at[8];
-    float r[8];
+  float acc[kUnits][8] = {};
+  for (i64 q = q0; q < q1; q += kEntries) {  // places first, then values, then sums
+    int at[kEntries];
+    float r[kEntries];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < kEntries; ++j) {
       const bool in = q + j < q1;
       at[j] = in ? a.pos[q + j] : INT_MAX;
       r[j] = in && a.val ? a.val[q + j] : 1.f;
     }
-    typename Raw<TI, kVec>::type v[8];
+    typename Raw<TI, kVec>::type v[kEntries][kUnits];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (at[j] < routed) v[j] = Raw<TI, kVec>::load(p + at[j] * a.p_stride);
+    for (int j = 0; j < kEntries; ++j)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+      for (int u = 0; u < kUnits; ++u)
+        if (at[j] < routed && c + u * kStep < a.width) v[j][u] = Raw<TI, kVec>::load(p + at[j] * a.p_stride + u * kStep);
+#pragma unroll
+    for (int j = 0; j < kEntries; ++j)
       if (at[j] < routed) {
-        float f[8];
-        Raw<TI, kVec>::values(v[j], f);
 #pragma unroll
-        for (int x = 0; x < kCols; ++x) acc[x] = fmaf(r[j], f[x], acc[x]);
+        for (int u = 0; u < kUnits; ++u) {
+          float f[8];
+          Raw<TI, kVec>::values(v[j][u], f);
+#pragma unroll
+          for (int x = 0; x < kCols; ++x) acc[u][x] = fmaf(r[j], f[x], acc[u][x]);
+        }
       }
   }
-  store_cols<TO, kVec>(static_cast<TO*>(a.y) + i * a.y_stride + c, acc);
+  TO* y = static_cast<TO*>(a.y) + i * a.y_stride + c;
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u)
+    if (c + u * kStep < a.width) {
+      if constexpr (kCols == 4) store4(y + u * kStep, acc[u]);
+      else store_cols<TO, kVec>(y + u * kStep, acc[u]);
+    }
 }
 
 // A warp per entry, in the order of the rows of R (so that a row's entries share its row of dY in cache).

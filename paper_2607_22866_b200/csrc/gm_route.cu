@@ -152,13 +152,14 @@ static int aligned_rows(gm_dense* M, Scratch* mem, int num_sms) {
   return fits ? GM_OK : pack(gm_dense(*M), mem, num_sms, M);
 }
 
-// A map of rows, 32 at a time.
-static int map_rows(CUtensorMap* map, gm_dense M, Scratch* mem, int num_sms) {
-  if (!map_fits(M, false)) GM_TRY(pack(gm_dense(M), mem, num_sms, &M));
+// A map of rows, `at_a_time` of them by 128 bytes; `rows`: what it lies over.
+static int map_rows(CUtensorMap* map, gm_dense* rows, uint32_t at_a_time, Scratch* mem, int num_sms) {
+  if (!map_fits(*rows, false)) GM_TRY(pack(gm_dense(*rows), mem, num_sms, rows));
+  const gm_dense& M = *rows;
   const i64 es = static_cast<i64>(elem_size(M.dtype));
   const uint64_t dims[2] = {static_cast<uint64_t>(M.n_cols), static_cast<uint64_t>(M.n_rows)};
   const uint64_t strides[1] = {static_cast<uint64_t>(M.n_rows > 1 ? M.row_stride * es : (M.n_cols * es + 15) / 16 * 16)};
-  const uint32_t box[2] = {static_cast<uint32_t>(kRowBytes / es), 32};
+  const uint32_t box[2] = {static_cast<uint32_t>(kRowBytes / es), at_a_time};
   return make_map(map, M.dtype, 2, M.data, dims, strides, box);
 }
 
@@ -190,6 +191,33 @@ static size_t product_smem(int E, bool bits8) {
   return kT5Smem + static_cast<size_t>(E + 1) * 8 + (bits8 ? kScaleSmem : 0);
 }
 static_assert(kT5Smem + (kRouteMaxCols + 1) * 8 + kScaleSmem <= kMostSmem, "fits a block's shared memory");
+
+// Whether clusters of kRouteBlocks fit the current device (more than 8 blocks are not promised), found out once.
+static bool wide_clusters() {
+  static std::atomic<unsigned long long> known{0}, fits{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (!(known.load() & bit)) {
+    int n = 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kRouteBlocks);
+    cfg.blockDim = dim3(kRouteThreads);
+    cfg.dynamicSmemBytes = kMostSmem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = kRouteBlocks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(reinterpret_cast<const void*>(k_route_plan), cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+        cudaOccupancyMaxActiveClusters(&n, k_route_plan, &cfg) == cudaSuccess && n > 0)
+      fits.fetch_or(bit);
+    cudaGetLastError();
+    known.fetch_or(bit);
+  }
+  return fits.load() & bit;
+}
 
 // A result of no terms: rows of zeros.
 static int zero_out(const gm_dense& M, cudaStream_t st) {
@@ -247,7 +275,7 @@ static int product(const gm_route* r, const gm_dense& X, bool by_entry, const gm
   GM_TRY(make_map(&map_w, V.dtype, 3, V.data, dims, strides, box));
   gm_dense rows = X;
   if (by_entry) {
-    GM_TRY(map_rows(&map_x, X, &mem, num_sms));
+    GM_TRY(map_rows(&map_x, &rows, 32, &mem, num_sms));
   } else {
     GM_TRY(aligned_rows(&rows, &mem, num_sms));
     map_x = map_w;  // (not used)
@@ -306,7 +334,10 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
   a.y = Y.data;
   a.y_stride = Y.row_stride;
   const bool vec = rows_aligned(P) && rows_aligned(Y);
-  const i64 per = kSumThreads * (vec ? 8 : 1), chunks = (a.width + per - 1) / per;
+  // eight loads in flight per thread: of as many entries as rows have on average, and the rest of other columns
+  const i64 mean = (r->nnz + r->n_rows - 1) / r->n_rows;
+  const int columns = !vec || mean > 4 ? 1 : mean > 2 ? 2 : 4;
+  const i64 per = kSumThreads * (vec ? columns * 16 / static_cast<i64>(elem_size(P.dtype)) : 1), chunks = (a.width + per - 1) / per;
   GM_TRY(sum_grid(chunks * r->n_rows, "sum"));
   const auto go = [&](auto kernel) {
     kernel<<<static_cast<unsigned>(chunks * r->n_rows), kSumThreads, 0, st>>>(a, static_cast<int>(chunks));
@@ -316,7 +347,8 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
   const auto typed2 = [&](auto* ti, auto* to) {
     using TI = std::remove_pointer_t<decltype(ti)>;
     using TO = std::remove_pointer_t<decltype(to)>;
-    return vec ? go(k_route_sum<TI, TO, true>) : go(k_route_sum<TI, TO, false>);
+    if (!vec) return go(k_route_sum<TI, TO, false, 1>);
+    return columns == 1 ? go(k_route_sum<TI, TO, true, 1>) : columns == 2 ? go(k_route_sum<TI, TO, true, 2>) : go(k_route_sum<TI, TO, true, 4>);
   };
   const auto typed = [&](auto* ti) {
     switch (Y.dtype) {
@@ -388,6 +420,9 @@ int gm_route_plan(const gm_csr* R, int64_t* offsets, int32_t* rows, int32_t* ord
     unsigned blocks = 1;
     while (blocks < kRouteBlocks && static_cast<i64>(blocks) * warps * 32 * 4 < r->nnz) blocks *= 2;
     const size_t smem = route_smem(r->E, warps);
+    int rc = allow_most_smem<k_route_plan>();
+    if (rc != GM_OK) return drop(rc);
+    if (blocks > 8 && !wide_clusters()) blocks = 8;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(warps * 32);
@@ -399,8 +434,6 @@ int gm_route_plan(const gm_csr* R, int64_t* offsets, int32_t* rows, int32_t* ord
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    int rc = allow_most_smem<k_route_plan>();
-    if (rc != GM_OK) return drop(rc);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, k_route_plan, r->row_ptr, R->col_idx, static_cast<int>(r->n_rows), r->nnz, r->E,
                                              r->offsets, r->rows, r->order, r->pos);
     if (e != cudaSuccess) return drop(fail(GM_ERR_CUDA, std::string("k_route_plan: ") + cudaGetErrorString(e)));
@@ -477,8 +510,14 @@ int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dens
     GM_TRY(device_facts_basic(&num_sms, &smem_optin));
     Scratch mem(st);
     gm_dense G = *dP, V = *X;
-    GM_TRY(aligned_rows(&G, &mem, num_sms));
-    GM_TRY(aligned_rows(&V, &mem, num_sms));
+    CUtensorMap map_p, map_x;
+    GM_TRY(map_rows(&map_p, &G, 64, &mem, num_sms));
+    if (by_entry) {
+      GM_TRY(map_rows(&map_x, &V, 64, &mem, num_sms));
+    } else {
+      GM_TRY(aligned_rows(&V, &mem, num_sms));
+      map_x = map_p;  // (not used)
+    }
     DwArgs a = {};
     a.offsets = route->offsets;
     a.rows = route->rows;
@@ -499,7 +538,7 @@ int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dens
     a.type = dP->dtype == GM_BF16 ? 1 : 0;
     a.err = route->err;
     const i64 tiles = static_cast<i64>(a.E) * ((a.n_m + kTileM - 1) / kTileM) * ((a.n_j + kTileN - 1) / kTileN);
-    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 320, kT5Smem, st, a); };
+    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 352, kT5Smem, st, map_p, map_x, a); };
     switch (dW->dtype) {
       case GM_F32: return by_entry ? go.template operator()<k_route_dw<false, float>>() : go.template operator()<k_route_dw<true, float>>();
       case GM_BF16: return by_entry ? go.template operator()<k_route_dw<false, __nv_bfloat16>>() : go.template operator()<k_route_dw<true, __nv_bfloat16>>();
@@ -650,7 +689,7 @@ int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_
     GM_TRY(make_map(&map_w, GM_E4M3, 3, V.data, dims, strides, box));
     gm_dense rows = *Xq;
     if (by_entry) {
-      GM_TRY(map_rows(&map_x, rows, &mem, num_sms));
+      GM_TRY(map_rows(&map_x, &rows, 32, &mem, num_sms));
     } else {
       GM_TRY(aligned_rows(&rows, &mem, num_sms));
       map_x = map_w;  // (not used)
