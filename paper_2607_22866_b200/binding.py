@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 from dataclasses import dataclass
 
@@ -84,12 +85,6 @@ class ExecStats(ctypes.Structure):
                 ("split_products", ctypes.c_int64)]
 
 
-class _Dense(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("n_blocks", ctypes.c_int64), ("n_rows", ctypes.c_int64), ("n_cols", ctypes.c_int64),
-                ("block_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("col_stride", ctypes.c_int64),
-                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
-
-
 _ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
 _FREE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p)
 
@@ -138,7 +133,7 @@ def load_library(install_torch_allocator: bool = True):
         lib.gm_plan_set_timing.argtypes = [vp, ctypes.c_int]
         lib.gm_plan_get_row_products.argtypes = [vp, vp, vp]
         lib.gm_row_products_noalloc.argtypes = [P(_CSR), P(_CSR), vp, vp]
-        D = P(_Dense)
+        D = vp  # a packed gm_dense
         lib.gm_route_plan.argtypes = [P(_CSR), vp, vp, vp, vp, vp, P(vp)]
         lib.gm_route_status.argtypes = [vp]
         lib.gm_route_destroy.argtypes = [vp]
@@ -348,19 +343,25 @@ _DTYPES = {torch.float32: 0, torch.float64: 1, torch.bfloat16: 2, torch.float16:
 _byref = ctypes.byref
 
 
-def _dense(t: torch.Tensor, where: str, device: torch.device) -> _Dense:
+_pack_dense = struct.Struct("=7q2i").pack  # a gm_dense
+
+
+def _dense(t: torch.Tensor, where: str, device: torch.device) -> bytes:
     if t.device != device:
         raise GmError(-1, where, f"a tensor on {t.device}, the others on {device}")
     shape, stride = t.shape, t.stride()
     if len(shape) == 2:
-        return _Dense(t.data_ptr(), 1, shape[0], shape[1], 0, stride[0], stride[1], _DTYPES.get(t.dtype, -1), 0)
-    return _Dense(t.data_ptr(), *shape, *stride, _DTYPES.get(t.dtype, -1), 0)
+        return _pack_dense(t.data_ptr(), 1, shape[0], shape[1], 0, stride[0], stride[1], _DTYPES.get(t.dtype, -1), 0)
+    return _pack_dense(t.data_ptr(), *shape, *stride, _DTYPES.get(t.dtype, -1), 0)
 
 
-def _result(t: torch.Tensor) -> _Dense:
+def _result(t: torch.Tensor, rows: int, cols: int) -> bytes:
     """A contiguous matrix that the call has just made."""
-    rows, cols = t.shape
-    return _Dense(t.data_ptr(), 1, rows, cols, 0, cols, 1, _DTYPES.get(t.dtype, -1), 0)
+    return _pack_dense(t.data_ptr(), 1, rows, cols, 0, cols, 1, _DTYPES.get(t.dtype, -1), 0)
+
+
+def _empty(like: torch.Tensor, rows: int, cols: int, dtype) -> torch.Tensor:
+    return like.new_empty((rows, cols)) if dtype is None else like.new_empty((rows, cols), dtype=dtype)
 
 
 def _dims(t: torch.Tensor, where: str, name: str, dims: int):
@@ -393,21 +394,29 @@ class Route:
     rows, order (nnz, int32): row and entry of R at every place; pos (nnz, int32): place of every entry.
     Keeps R alive, whose row_ptr and val it borrows."""
 
-    def __init__(self, handle, R: DeviceCSR, stream: int, offsets: torch.Tensor, places: torch.Tensor):
-        self._h, self.R, self._stream, self.offsets, self._places = handle, R, stream, offsets, places
-        self.n_rows, self.n_cols, self.nnz, self.device = R.n_rows, R.n_cols, R.nnz, offsets.device
+    def __init__(self, handle, R: DeviceCSR, stream: int, memory: torch.Tensor):
+        self._h, self.R, self._stream, self._memory = handle, R, stream, memory
+        self.n_rows, self.n_cols, self.nnz, self.device = R.n_rows, R.n_cols, R.nnz, memory.device
+
+    def _places(self, k: int) -> torch.Tensor:
+        first = 2 * (self.n_cols + 1) + k * self.nnz
+        return self._memory[first: first + self.nnz]
+
+    @property
+    def offsets(self) -> torch.Tensor:
+        return self._memory[: 2 * (self.n_cols + 1)].view(torch.int64)
 
     @property
     def rows(self) -> torch.Tensor:
-        return self._places[0]
+        return self._places(0)
 
     @property
     def order(self) -> torch.Tensor:
-        return self._places[1]
+        return self._places(1)
 
     @property
     def pos(self) -> torch.Tensor:
-        return self._places[2]
+        return self._places(2)
 
     def status(self):
         """Raises GmError(GM_ERR_TIMEOUT) if a kernel of a finished call on this route gave up a wait."""
@@ -417,7 +426,7 @@ class Route:
         stream = torch._C._cuda_getCurrentRawStream(self.device.index)
         if stream != self._stream:  # not the one its memory belongs to
             s = torch.cuda.current_stream(self.device)
-            for t in (self.offsets, self._places, self.R.row_ptr, self.R.val):
+            for t in (self._memory, self.R.row_ptr, self.R.val):
                 t.record_stream(s)
         return stream
 
@@ -447,11 +456,12 @@ def route_plan(R: DeviceCSR, stream=None) -> Route:
         raise GmError(-1, where, "R's arrays are on different devices")
     if R.n_cols < 0 or R.nnz < 0 or R.row_ptr.numel() < R.n_rows + 1 or R.col.numel() < R.nnz or R.val.numel() < R.nnz:
         raise GmError(-1, where, "R's arrays are shorter than its sizes say")
-    offsets = torch.empty(R.n_cols + 1, dtype=torch.int64, device=device)
-    places = torch.empty((3, R.nnz), dtype=torch.int32, device=device)
-    st, h, at = torch._C._cuda_getCurrentRawStream(device.index), ctypes.c_void_p(), places.data_ptr()
-    _check(load_library().gm_route_plan(_byref(R._struct()), offsets.data_ptr(), at, at + 4 * R.nnz, at + 8 * R.nnz, st, _byref(h)), where)
-    return Route(h, R, st, offsets, places)
+    n_off = 2 * (R.n_cols + 1)
+    memory = torch.empty(n_off + 3 * R.nnz, dtype=torch.int32, device=device)
+    st, h, at = torch._C._cuda_getCurrentRawStream(device.index), ctypes.c_void_p(), memory.data_ptr()
+    rows = at + 4 * n_off
+    _check(load_library().gm_route_plan(_byref(R._struct()), at, rows, rows + 4 * R.nnz, rows + 8 * R.nnz, st, _byref(h)), where)
+    return Route(h, R, st, memory)
 
 
 def route_product(route: Route, X: torch.Tensor, W: torch.Tensor, by_entry: bool = False, dtype=None, stream=None) -> torch.Tensor:
@@ -462,9 +472,10 @@ def route_product(route: Route, X: torch.Tensor, W: torch.Tensor, by_entry: bool
         return _there(route_product, device, stream, route, X, W, by_entry, dtype)
     _dims(X, where, "X", 2)
     _dims(W, where, "W", 3)
-    P = torch.empty((route.nnz, W.shape[1]), dtype=dtype or X.dtype, device=device)
-    _check(load_library().gm_route_product(route._h, _byref(_dense(X, where, device)), by_entry, _byref(_dense(W, where, device)),
-                                           _byref(_result(P)), route._current_stream()), where)
+    N = W.shape[1]
+    P = _empty(X, route.nnz, N, dtype)
+    _check(load_library().gm_route_product(route._h, _dense(X, where, device), by_entry, _dense(W, where, device),
+                                           _result(P, route.nnz, N), route._current_stream()), where)
     return P
 
 
@@ -475,9 +486,10 @@ def route_product_dx(route: Route, dP: torch.Tensor, W: torch.Tensor, by_entry: 
         return _there(route_product_dx, device, stream, route, dP, W, by_entry, dtype)
     _dims(dP, where, "dP", 2)
     _dims(W, where, "W", 3)
-    dX = torch.empty((route.nnz if by_entry else route.n_rows, W.shape[2]), dtype=dtype or dP.dtype, device=device)
-    _check(load_library().gm_route_product_dx(route._h, _byref(_dense(dP, where, device)), _byref(_dense(W, where, device)), by_entry,
-                                              _byref(_result(dX)), route._current_stream()), where)
+    rows, K = route.nnz if by_entry else route.n_rows, W.shape[2]
+    dX = _empty(dP, rows, K, dtype)
+    _check(load_library().gm_route_product_dx(route._h, _dense(dP, where, device), _dense(W, where, device), by_entry,
+                                              _result(dX, rows, K), route._current_stream()), where)
     return dX
 
 
@@ -489,8 +501,8 @@ def route_product_dw(route: Route, dP: torch.Tensor, X: torch.Tensor, by_entry: 
     _dims(dP, where, "dP", 2)
     _dims(X, where, "X", 2)
     dW = torch.empty((route.n_cols, dP.shape[1], X.shape[1]), dtype=dtype or dP.dtype, device=device)
-    _check(load_library().gm_route_product_dw(route._h, _byref(_dense(dP, where, device)), _byref(_dense(X, where, device)), by_entry,
-                                              _byref(_dense(dW, where, device)), route._current_stream()), where)
+    _check(load_library().gm_route_product_dw(route._h, _dense(dP, where, device), _dense(X, where, device), by_entry,
+                                              _dense(dW, where, device), route._current_stream()), where)
     return dW
 
 
@@ -500,8 +512,8 @@ def route_sum(route: Route, P: torch.Tensor, weighted: bool = True, dtype=None, 
     if not _is_here(where, device, stream):
         return _there(route_sum, device, stream, route, P, weighted, dtype)
     _dims(P, where, "P", 2)
-    Y = torch.empty((route.n_rows, P.shape[1]), dtype=dtype or P.dtype, device=device)
-    _check(load_library().gm_route_sum(route._h, _byref(_dense(P, where, device)), weighted, _byref(_result(Y)), route._current_stream()), where)
+    Y = _empty(P, route.n_rows, P.shape[1], dtype)
+    _check(load_library().gm_route_sum(route._h, _dense(P, where, device), weighted, _result(Y, route.n_rows, P.shape[1]), route._current_stream()), where)
     return Y
 
 
@@ -512,9 +524,9 @@ def route_sum_grads(route: Route, dY: torch.Tensor, P: torch.Tensor, stream=None
         return _there(route_sum_grads, device, stream, route, dY, P)
     _dims(dY, where, "dY", 2)
     _dims(P, where, "P", 2)
-    dP = torch.empty((route.nnz, P.shape[1]), dtype=P.dtype, device=device)
+    dP = _empty(P, route.nnz, P.shape[1], None)
     dval = torch.empty(route.nnz, dtype=torch.float32, device=device)
-    _check(load_library().gm_route_sum_grads(route._h, _byref(_dense(dY, where, device)), _byref(_dense(P, where, device)), _byref(_result(dP)),
+    _check(load_library().gm_route_sum_grads(route._h, _dense(dY, where, device), _dense(P, where, device), _result(dP, route.nnz, P.shape[1]),
                                              dval.data_ptr(), route._current_stream()), where)
     return dP, dval
 
@@ -532,8 +544,8 @@ def block_quantize(X: torch.Tensor, block_rows: int = 1, stream=None) -> tuple[t
         raise GmError(-2, where, f"X: {len(shape)} dimensions instead of 2 or 3")
     Q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
     S = torch.empty((*shape[:-2], -(-shape[-2] // block_rows), -(-shape[-1] // 128)), dtype=torch.float32, device=device)
-    _check(load_library().gm_block_quantize(_byref(_dense(X, where, device)), block_rows, _byref(_dense(Q, where, device)),
-                                            _byref(_dense(S, where, device)), torch._C._cuda_getCurrentRawStream(device.index)), where)
+    _check(load_library().gm_block_quantize(_dense(X, where, device), block_rows, _dense(Q, where, device),
+                                            _dense(S, where, device), torch._C._cuda_getCurrentRawStream(device.index)), where)
     return Q, S
 
 
@@ -546,8 +558,9 @@ def route_product_scaled(route: Route, Xq: torch.Tensor, Xs: torch.Tensor, Wq: t
         return _there(route_product_scaled, device, stream, route, Xq, Xs, Wq, Ws, by_entry, dtype)
     for t, name, dims in ((Xq, "Xq", 2), (Xs, "Xs", 2), (Wq, "Wq", 3), (Ws, "Ws", 3)):
         _dims(t, where, name, dims)
-    P = torch.empty((route.nnz, Wq.shape[1]), dtype=dtype, device=device)
-    _check(load_library().gm_route_product_scaled(route._h, _byref(_dense(Xq, where, device)), _byref(_dense(Xs, where, device)), by_entry,
-                                                  _byref(_dense(Wq, where, device)), _byref(_dense(Ws, where, device)), _byref(_result(P)),
+    N = Wq.shape[1]
+    P = _empty(Xq, route.nnz, N, dtype)
+    _check(load_library().gm_route_product_scaled(route._h, _dense(Xq, where, device), _dense(Xs, where, device), by_entry,
+                                                  _dense(Wq, where, device), _dense(Ws, where, device), _result(P, route.nnz, N),
                                                   route._current_stream()), where)
     return P

@@ -9,7 +9,7 @@
 #pragma once
 #include <cooperative_groups.h>
 
-#include "gm_common.cuh"
+#include "gm_t5.cuh"
 
 namespace gm {
 
@@ -72,7 +72,9 @@ __global__ void __launch_bounds__(kRouteThreads, 1) k_route_plan(const i64* __re
   u32* cnt = route_sm + static_cast<size_t>(warp) * bins;   // this warp's entries per column, then its next places
   u32* sum = route_sm + static_cast<size_t>(warps) * bins;  // this block's entries per column: read by the others
   u32* base = sum + bins;                                   // first place of this block's entries of a column
+  grid_launch_next();
   for (int e = lane; e < bins; e += 32) cnt[e] = 0;
+  grid_wait();
   const i64 n_warps = static_cast<i64>(gridDim.x) * warps, per = (nnz + n_warps - 1) / n_warps;
   const i64 q0 = min(nnz, (static_cast<i64>(blockIdx.x) * warps + warp) * per), q1 = min(nnz, q0 + per);
   // the first columns and their rows stay in registers for the second walk

@@ -113,6 +113,7 @@ __device__ __forceinline__ char* t5_align(char* p) { return p + ((1024 - (smem_u
 
 // full_arrivals: on the leader's barrier of a stage, by both blocks;  result_warps: of one block.
 __device__ __forceinline__ void t5_begin(T5Block* b, int full_arrivals, int result_warps) {
+  grid_launch_next();
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(&b->full[i], full_arrivals); mbar_init(&b->empty[i], 1); mbar_init(&b->copied[i], kCopyThreads); }
     for (int i = 0; i < 2; ++i) { mbar_init(&b->sums_full[i], 1); mbar_init(&b->sums_empty[i], 2 * result_warps); }
@@ -313,6 +314,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const u32 rank = cluster_rank();
   t5_begin(b, kGather ? 3 : 1, 4);
+  grid_wait();
   list_parts(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 63) / 64;
   const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
@@ -407,6 +409,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
   if (threadIdx.x == 32)
     for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&sb->full[i], 1); mbar_init(&sb->empty[i], 8); }
   t5_begin(b, kGather ? 3 : 1, 8);
+  grid_wait();
   list_parts(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 127) / 128;
   const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
@@ -572,6 +575,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const u32 rank = cluster_rank();
   t5_begin(b, 3, 4);
+  grid_wait();
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_jt = (a.n_j + kTileN - 1) / kTileN, n_per = n_mt * n_jt;
   const i64 n_tiles = static_cast<i64>(a.E) * n_per;
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
@@ -748,6 +752,8 @@ template <typename T>
 __global__ void k_route_pack(const T* __restrict__ src, i64 block_stride, i64 row_stride, i64 col_stride, i64 n_blocks, i64 n_rows,
                              i64 n_cols, i64 padded, T* __restrict__ dst) {
   const i64 total = n_blocks * n_rows * padded;
+  grid_launch_next();
+  grid_wait();
   for (i64 i = static_cast<i64>(blockIdx.x) * blockDim.x + threadIdx.x; i < total; i += static_cast<i64>(gridDim.x) * blockDim.x) {
     const i64 c = i % padded, br = i / padded, r = br % n_rows, blk = br / n_rows;
     dst[i] = c < n_cols ? src[blk * block_stride + r * row_stride + c * col_stride] : T(0);

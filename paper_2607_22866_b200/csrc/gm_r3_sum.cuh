@@ -126,7 +126,9 @@ __global__ void __launch_bounds__(kSumThreads) k_route_sum(const SumArgs a, int 
   constexpr int kCols = kVec ? 16 / sizeof(TI) : 1, kEntries = 8 / kUnits, kStep = kSumThreads * kCols;
   const i64 i = blockIdx.x / n_chunks;
   const int c = static_cast<int>(blockIdx.x % n_chunks) * kUnits * kStep + threadIdx.x * kCols;
+  grid_launch_next();
   if (c >= a.width) return;
+  grid_wait();
   const i64 q0 = max(static_cast<i64>(0), a.row_ptr[i]), q1 = min(a.entries, a.row_ptr[i + 1]);
   const int routed = static_cast<int>(a.offsets[a.E]);
   const TI* p = static_cast<const TI*>(a.p) + c;
@@ -173,7 +175,9 @@ __global__ void __launch_bounds__(256) k_route_sum_grads(const SumArgs a, TD* __
   constexpr int kCols = kVec ? 8 : 1;
   const int lane = threadIdx.x & 31;
   const i64 q = static_cast<i64>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  grid_launch_next();
   if (q >= a.entries) return;
+  grid_wait();
   const int at = a.pos[q];
   TD* out = dp + at * dp_stride;
   if (at >= a.offsets[a.E]) {  // routed nowhere

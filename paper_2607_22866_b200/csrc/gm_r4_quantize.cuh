@@ -118,6 +118,8 @@ __global__ void __launch_bounds__(256) k_quantize_rows(const QuantArgs a) {
   uint4 x[kQuantAhead];
   unsigned char* to[kQuantAhead];
   int col[kQuantAhead];
+  grid_launch_next();
+  grid_wait();
 #pragma unroll
   for (int j = 0; j < kQuantAhead; ++j) {
     const i64 unit = first + 16 * j;
@@ -162,6 +164,8 @@ __global__ void __launch_bounds__(256) k_quantize_tiles(const QuantArgs a, int r
   const int c = cg * 128 + (threadIdx.x & 15) * 8, r = threadIdx.x >> 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const T* x = static_cast<const T*>(a.x) + blk * a.x_block;
   uint4 v[8];
+  grid_launch_next();
+  grid_wait();
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const i64 row = r0 + r + 16 * j;

@@ -29,6 +29,27 @@ struct gm_route {
 
 namespace gm {
 
+// A launch that may begin while the kernel before it in the stream ends (see grid_wait); cluster: blocks per cluster, 0 = as the
+// kernel says.
+template <typename... P, typename... A>
+static int launch(void (*kernel)(P...), i64 blocks, int threads, size_t smem, cudaStream_t st, unsigned cluster, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster ? 2 : 1;
+  GM_CUDA(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
+  return GM_OK;
+}
+
 static size_t elem_size(int dtype) {
   switch (dtype) {
     case GM_F32: return 4;
@@ -122,13 +143,11 @@ static int pack(const gm_dense& M, Scratch* mem, int num_sms, gm_dense* out) {
   if (!p) return fail(GM_ERR_OOM, "no room for an aligned copy of " + std::to_string(bytes) + " bytes");
   const i64 total = M.n_blocks * M.n_rows * padded;
   const unsigned grid = static_cast<unsigned>(std::min<i64>((total + 255) / 256, static_cast<i64>(num_sms) * 16));
-  if (es == 2)
-    k_route_pack<uint16_t><<<grid, 256, 0, mem->st>>>(static_cast<const uint16_t*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<uint16_t*>(p));
-  else if (es == 4)
-    k_route_pack<uint32_t><<<grid, 256, 0, mem->st>>>(static_cast<const uint32_t*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<uint32_t*>(p));
-  else
-    k_route_pack<uint8_t><<<grid, 256, 0, mem->st>>>(static_cast<const uint8_t*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<uint8_t*>(p));
-  GM_CUDA(cudaGetLastError());
+  const auto go = [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    return launch(k_route_pack<T>, grid, 256, 0, mem->st, 0, static_cast<const T*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<T*>(p));
+  };
+  GM_TRY(es == 2 ? go(static_cast<uint16_t*>(nullptr)) : es == 4 ? go(static_cast<uint32_t*>(nullptr)) : go(static_cast<uint8_t*>(nullptr)));
   *out = M;
   out->data = p;
   out->col_stride = 1;
@@ -232,9 +251,7 @@ static int zero_out(const gm_dense& M, cudaStream_t st) {
 template <auto kernel, typename... A>
 static int launch_t5(i64 tiles, int num_sms, int threads, size_t smem, cudaStream_t st, const A&... args) {
   GM_TRY(allow_most_smem<kernel>());
-  kernel<<<static_cast<unsigned>(2 * std::max<i64>(1, std::min<i64>(tiles, num_sms / 2))), threads, smem, st>>>(args...);
-  GM_CUDA(cudaGetLastError());
-  return GM_OK;
+  return launch(kernel, 2 * std::max<i64>(1, std::min<i64>(tiles, num_sms / 2)), threads, smem, st, 0, args...);
 }
 
 // out[p, m] = sum_k B[e(p)](m, k) X[x row of p, k];  w_transposed: B's rows are W's columns.
@@ -340,9 +357,7 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
   const i64 per = kSumThreads * (vec ? columns * 16 / static_cast<i64>(elem_size(P.dtype)) : 1), chunks = (a.width + per - 1) / per;
   GM_TRY(sum_grid(chunks * r->n_rows, "sum"));
   const auto go = [&](auto kernel) {
-    kernel<<<static_cast<unsigned>(chunks * r->n_rows), kSumThreads, 0, st>>>(a, static_cast<int>(chunks));
-    GM_CUDA(cudaGetLastError());
-    return static_cast<int>(GM_OK);
+    return launch(kernel, chunks * r->n_rows, kSumThreads, 0, st, 0, a, static_cast<int>(chunks));
   };
   const auto typed2 = [&](auto* ti, auto* to) {
     using TI = std::remove_pointer_t<decltype(ti)>;
@@ -423,20 +438,9 @@ int gm_route_plan(const gm_csr* R, int64_t* offsets, int32_t* rows, int32_t* ord
     int rc = allow_most_smem<k_route_plan>();
     if (rc != GM_OK) return drop(rc);
     if (blocks > 8 && !wide_clusters()) blocks = 8;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3(warps * 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = blocks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_route_plan, r->row_ptr, R->col_idx, static_cast<int>(r->n_rows), r->nnz, r->E,
-                                             r->offsets, r->rows, r->order, r->pos);
-    if (e != cudaSuccess) return drop(fail(GM_ERR_CUDA, std::string("k_route_plan: ") + cudaGetErrorString(e)));
+    rc = launch(k_route_plan, blocks, warps * 32, smem, st, blocks, r->row_ptr, R->col_idx, static_cast<int>(r->n_rows), r->nnz, r->E,
+                r->offsets, r->rows, r->order, r->pos);
+    if (rc != GM_OK) return drop(rc);
     *route_out = r;
     return GM_OK;
   });
@@ -597,9 +601,7 @@ int gm_route_sum_grads(const gm_route* route, const gm_dense* dY, const gm_dense
     const auto typed = [&](auto* tag) {
       using T = std::remove_pointer_t<decltype(tag)>;
       const auto kernel = vec ? k_route_sum_grads<T, T, true> : k_route_sum_grads<T, T, false>;
-      kernel<<<static_cast<unsigned>((route->nnz + 7) / 8), 256, 0, st>>>(a, static_cast<T*>(dP->data), dP->row_stride, dval);
-      GM_CUDA(cudaGetLastError());
-      return static_cast<int>(GM_OK);
+      return launch(kernel, (route->nnz + 7) / 8, 256, 0, st, 0, a, static_cast<T*>(dP->data), dP->row_stride, dval);
     };
     switch (dY->dtype) {
       case GM_F32: return typed(static_cast<float*>(nullptr));
@@ -643,10 +645,9 @@ int gm_block_quantize(const gm_dense* X, int block_rows, const gm_dense* Q, cons
     GM_TRY(sum_grid(blocks, "quantize"));
     const auto typed = [&](auto* tag) {
       using T = std::remove_pointer_t<decltype(tag)>;
-      if (block_rows == 1) (flat ? k_quantize_rows<T, true, true> : vec ? k_quantize_rows<T, true, false> : k_quantize_rows<T, false, false>)<<<static_cast<unsigned>(blocks), 256, 0, st>>>(a);
-      else (vec ? k_quantize_tiles<T, true> : k_quantize_tiles<T, false>)<<<static_cast<unsigned>(blocks), 256, 0, st>>>(a, static_cast<int>(rg));
-      GM_CUDA(cudaGetLastError());
-      return static_cast<int>(GM_OK);
+      if (block_rows == 1)
+        return launch(flat ? k_quantize_rows<T, true, true> : vec ? k_quantize_rows<T, true, false> : k_quantize_rows<T, false, false>, blocks, 256, 0, st, 0, a);
+      return launch(vec ? k_quantize_tiles<T, true> : k_quantize_tiles<T, false>, blocks, 256, 0, st, 0, a, static_cast<int>(rg));
     };
     return X->dtype == GM_BF16 ? typed(static_cast<__nv_bfloat16*>(nullptr)) : typed(static_cast<__half*>(nullptr));
   });

@@ -7,6 +7,11 @@
 
 namespace gm {
 
+// Kernels of the routed products are launched while the one before them in the stream still runs (programmatic dependent launch):
+// what they do before grid_wait() touches no global memory, and behind it all that was queued before is done.
+__device__ __forceinline__ void grid_launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Polls of a barrier before a wait gives up: a failed try_wait has itself waited for a while, so this is far above any
 // wait that ends (the longest is for one tile's products, under 2 ms).
 constexpr int kT5SpinLimit = 1 << 22;
