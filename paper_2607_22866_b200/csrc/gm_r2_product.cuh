@@ -26,7 +26,6 @@ constexpr int kRowBytes = 128;     // of one operand row in a stage: 64 values o
 constexpr int kStages = 6;
 constexpr int kHalf = 128 * kRowBytes;  // one block's share of an operand in a stage
 constexpr int kStage = 2 * kHalf;
-constexpr int kCopyThreads = 128;  // that fetch rows by index
 constexpr u32 kTmemColumns = 512;
 
 struct ProductArgs {
@@ -66,12 +65,16 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
+// Which rows of X a tile needs is itself copied into shared memory, during the tile before and by the warp that needs it.
+constexpr int kIndexSlot = 128;  // one block's rows of a tile
+
 // The barriers and the place in tensor memory of a block, behind its stages.
 struct T5Block {
   u64 full[kStages], empty[kStages], copied[kStages];
   u64 sums_full[2], sums_empty[2], drain;
   u32 tmem;
   u32 scan_tmp[34];
+  int index[2 * kIndexSlot];
 };
 
 // Places of each column, cut into parts of at most kTileN places that differ by less than 32 in size.
@@ -112,10 +115,10 @@ __device__ __forceinline__ Part part_at(const int* off, const int* part, int E, 
 __device__ __forceinline__ char* t5_align(char* p) { return p + ((1024 - (smem_u32(p) & 1023)) & 1023); }
 
 // full_arrivals: on the leader's barrier of a stage, by both blocks;  result_warps: of one block.
-__device__ __forceinline__ void t5_begin(T5Block* b, int full_arrivals, int result_warps) {
+__device__ __forceinline__ void t5_begin(T5Block* b, int full_arrivals, int result_warps, int copy_threads) {
   grid_launch_next();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&b->full[i], full_arrivals); mbar_init(&b->empty[i], 1); mbar_init(&b->copied[i], kCopyThreads); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&b->full[i], full_arrivals); mbar_init(&b->empty[i], 1); mbar_init(&b->copied[i], copy_threads); }
     for (int i = 0; i < 2; ++i) { mbar_init(&b->sums_full[i], 1); mbar_init(&b->sums_empty[i], 2 * result_warps); }
     mbar_init(&b->drain, 1);
     mbar_fence_init();
@@ -156,9 +159,11 @@ struct CopyQueue {
   }
   __device__ __forceinline__ void done() {  // the stage's copies are all issued
     copy_arrive(&b->copied[issued % kStages]);
+    copy_commit();
     ++issued;
   }
 };
+
 __device__ __forceinline__ bool hand_over(T5Block* b, u32 stage) {
   if (!t5_wait(&b->copied[stage % kStages], (stage / kStages) & 1)) return false;
   fence_to_matrix();
@@ -168,28 +173,48 @@ __device__ __forceinline__ bool hand_over(T5Block* b, u32 stage) {
 
 // The rows of X of one block's half of the places, for every tile and stage: eight lanes have a row of a stage.
 template <int kValueBytes>
-__device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u32 stage0, const int* off, const int* part, i64 n_tiles, int n_mt,
-                                            int thread) {
+__device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u32 stage0, int* index, const int* off, const int* part, i64 n_tiles,
+                                            int n_mt, int thread) {
   CopyQueue queue(b);
-  const int n_kb = (a.n_k * kValueBytes + kRowBytes - 1) / kRowBytes, c = thread & 7, r0 = thread >> 3;
+  const int n_kb = (a.n_k * kValueBytes + kRowBytes - 1) / kRowBytes, c = thread & 7, r0 = thread >> 3, lane = thread & 31;
   const u32 at = kHalf + r0 * kRowBytes + ((c ^ (r0 & 7)) << 4);  // (rows r0 + 16 i: the same swizzle)
+  constexpr int kApart = 16, kRows = 8;  // a thread's rows: r0 + 16 i
+  const int my_row = (thread >> 5) * 4 + (lane & 3) + kApart * (lane >> 2);  // the one whose index this lane brings in for its warp
   const i64 width = static_cast<i64>(a.n_k) * kValueBytes;
   const u32 rank = cluster_rank();
+  const i64 pairs = gridDim.x >> 1;
+  const auto bring_rows = [&](i64 id, int slot) {
+    if (id >= n_tiles) return;
+    const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+    const int half = round32(t.n) / 2, p = rank * half + my_row;
+    int* to = index + slot * kIndexSlot + my_row;
+    if (my_row < half && p < t.n) copy4(smem_u32(to), a.rows + t.first + p);
+    else *to = -1;
+  };
   bool ok = true;
-  for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+  int slot = 0;
+  bring_rows(blockIdx.x >> 1, 0);
+  copy_commit();
+  for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += pairs, slot ^= 1) {
     const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
     const int half = round32(t.n) / 2;
-    const char* src[8];
+    // this tile's rows came with the last tile's first stage
+    if (n_kb > kStages && id >= pairs) copy_wait<kStages>();
+    else copy_wait_all();
+    __syncwarp();
+    const char* src[kRows];
     u32 there = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = r0 + 16 * i, p = rank * half + r;
+    for (int i = 0; i < kRows; ++i) {
+      const int r = index[slot * kIndexSlot + r0 + kApart * i];
       src[i] = a.x;
-      if (r < half && p < t.n) {
-        src[i] += a.rows[t.first + p] * a.x_stride;
+      if (r >= 0) {
+        src[i] += r * a.x_stride;
         there |= 1u << i;
       }
     }
+    __syncwarp();
+    bring_rows(id + pairs, slot ^ 1);
     for (int kb = 0; kb < n_kb; ++kb) {
       ok = queue.slot_free();
       if (!ok) break;
@@ -198,8 +223,8 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
       const u32 bytes = static_cast<u32>(max(static_cast<i64>(0), min(static_cast<i64>(16), width - x)));
       const i64 from = bytes ? x : 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (r0 + 16 * i < half) copy16(dst + i * 16 * kRowBytes, src[i] + from, there >> i & 1 ? bytes : 0);
+      for (int i = 0; i < kRows; ++i)
+        if (r0 + kApart * i < half) copy16(dst + i * kApart * kRowBytes, src[i] + from, there >> i & 1 ? bytes : 0);
       queue.done();
     }
   }
@@ -257,13 +282,16 @@ __device__ __forceinline__ void zero_rows(TO* out, i64 stride, i64 p0, i64 p1, i
     for (int m = threadIdx.x; m < width; m += blockDim.x) out[p * stride + m] = from_float<TO>(0.f);
 }
 
-// Lane = row m of the tile, v[j] = place j of a run of 32: out[(p + j) * stride + m].
+// Lane = row m of the tile, v[j] = place j of a run of 16: out[(p + j) * stride + m].
 template <typename TO>
-__device__ __forceinline__ void store_places(TO* __restrict__ out, i64 stride, i64 p, int n, int m, int n_m, const u32 (&v)[32]) {
+__device__ __forceinline__ void store_places(TO* __restrict__ out, i64 stride, i64 p, int n, int m, int n_m, const u32 (&v)[16]) {
   if (m < n_m) {
+    TO* to = out + p * stride + m;
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j < n) out[(p + j) * stride + m] = from_float<TO>(__uint_as_float(v[j]));
+    for (int j = 0; j < 16; ++j) {
+      if (j < n) *to = from_float<TO>(__uint_as_float(v[j]));
+      to += stride;
+    }
   }
 }
 
@@ -313,7 +341,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
   int* part = off + a.E + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const u32 rank = cluster_rank();
-  t5_begin(b, kGather ? 3 : 1, 4);
+  t5_begin(b, kGather ? 3 : 1, 4, 128);
   grid_wait();
   list_parts(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 63) / 64;
@@ -364,10 +392,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
       ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done >> 1) & 1));
       if (!ok) break;
       t5_fence_after();
-      for (int c = 0; c < t.n; c += 32) {
-        u32 v[32];
-        t5_ld32(v, tmem + buf * kTileN + c + (static_cast<u32>(quad * 32) << 16));
-        t5_wait_ld();
+      for (int c = 0; c < t.n; c += 16) {
+        u32 v[16];
+        t5_ld16(v, tmem + buf * kTileN + c + (static_cast<u32>(quad * 32) << 16));
+        t5_wait_ld16(v);
         store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + c, t.n - c, m, a.n_m, v);
       }
       t5_fence_before();
@@ -375,7 +403,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   } else if (warp < 10) {
-    gather_rows<2>(a, b, stage0, off, part, n_tiles, n_mt, threadIdx.x - 192);
+    gather_rows<2>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 192);
   } else {
     if (lane == 0) hand_over_rows(a, b, n_tiles, n_kb);
     __syncwarp();
@@ -408,7 +436,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
   const u32 rank = cluster_rank();
   if (threadIdx.x == 32)
     for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&sb->full[i], 1); mbar_init(&sb->empty[i], 8); }
-  t5_begin(b, kGather ? 3 : 1, 8);
+  t5_begin(b, kGather ? 3 : 1, 8, 128);
   grid_wait();
   list_parts(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 127) / 128;
@@ -545,39 +573,80 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
       }
       if (ok) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          u32 v[32];
+        for (int c = 0; c < 8; ++c) {
+          u32 v[16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(v[2 * j]), "=r"(v[2 * j + 1]) : "l"(acc[c * 16 + j]));
-          if (c * 32 < mine)
-            store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + half * 128 + c * 32, mine - c * 32, m, a.n_m, v);
+          for (int j = 0; j < 8; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(v[2 * j]), "=r"(v[2 * j + 1]) : "l"(acc[c * 8 + j]));
+          if (c * 16 < mine)
+            store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + half * 128 + c * 16, mine - c * 16, m, a.n_m, v);
         }
       }
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(48));
-    gather_rows<1>(a, b, stage0, off, part, n_tiles, n_mt, threadIdx.x - 384);
+    gather_rows<1>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 384);
   }
   t5_end(tmem);
 }
 
 // Both operands lie with the reduction (64 places a stage) across their rows.  Stages of 64 places of one column come by tensor map (dP, and X
-// with a row per place); rows by index, and a column's last places, 16 bytes at a time by four warps: what lies behind the last place is
+// with a row per place); rows by index, and a column's last places, 16 bytes at a time by eight warps: what lies behind the last place is
 // not read but zero, so that a sum ends inside a stage whatever its neighbour holds.
-// Warps: 0 copies by tensor map, 1 matrix instructions, 2-5 results, 6-9 copies, 10 hands those over.
+// Warps: 0 copies by tensor map, 1 matrix instructions, 2-5 results, 6-13 copies, 14 hands those over.
+// A tile of dW, and a walk over those of a pair of blocks that have places.
+struct DwTile {
+  i64 id;
+  int p0, p1, m0, j0, half;  // half: columns of X per block, 128 or 64
+};
+struct DwWalk {
+  const DwArgs& a;
+  const int* off;
+  int n_mt, n_per;
+  i64 n_tiles;
+  __device__ __forceinline__ DwWalk(const DwArgs& args, const int* offsets) : a(args), off(offsets) {
+    n_mt = (a.n_m + kTileM - 1) / kTileM;
+    n_per = n_mt * ((a.n_j + kTileN - 1) / kTileN);
+    n_tiles = static_cast<i64>(a.E) * n_per;
+  }
+  __device__ __forceinline__ DwTile at(i64 id) const {
+    const int e = static_cast<int>(id / n_per), rest = static_cast<int>(id - static_cast<i64>(e) * n_per), j = rest / n_mt;
+    DwTile t;
+    t.id = id;
+    t.p0 = off[e];
+    t.p1 = off[e + 1];
+    t.m0 = (rest - j * n_mt) * kTileM;
+    t.j0 = j * kTileN;
+    t.half = a.n_j - t.j0 > 128 ? 128 : 64;
+    return t;
+  }
+  __device__ __forceinline__ DwTile first() const { return settle(blockIdx.x >> 1); }
+  __device__ __forceinline__ DwTile next(const DwTile& t) const { return settle(t.id + (gridDim.x >> 1)); }
+  __device__ __forceinline__ DwTile settle(i64 id) const {  // the next tile with places; id >= n_tiles: none
+    for (; id < n_tiles; id += gridDim.x >> 1) {
+      const DwTile t = at(id);
+      if (t.p0 < t.p1) return t;
+    }
+    DwTile none = {};
+    none.id = id;
+    return none;
+  }
+};
+
 template <bool kGather, typename TO>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
     k_route_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const DwArgs a) {
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
   T5Block* b = reinterpret_cast<T5Block*>(stages + kStages * kStage);
+  int* off = reinterpret_cast<int*>(b + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const u32 rank = cluster_rank();
-  t5_begin(b, 3, 4);
+  t5_begin(b, 3, 4, 256);
   grid_wait();
-  const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_jt = (a.n_j + kTileN - 1) / kTileN, n_per = n_mt * n_jt;
-  const i64 n_tiles = static_cast<i64>(a.E) * n_per;
+  for (int e = threadIdx.x; e <= a.E; e += blockDim.x) off[e] = static_cast<int>(a.offsets[e]);
+  __syncthreads();
+  const DwWalk walk(a, off);
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
   constexpr u32 kBlock = 64 * kRowBytes;  // 64 places of 64 values
 
@@ -585,24 +654,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
     if (lane == 0) {
       u32 it = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-        const int e = static_cast<int>(id / n_per), rest = static_cast<int>(id % n_per);
-        const int j0 = rest / n_mt * kTileN, half = a.n_j - j0 > 128 ? 128 : 64;
-        const int m = rest % n_mt * kTileM + rank * 128, j = j0 + rank * half;
-        const int p0 = static_cast<int>(a.offsets[e]), p1 = static_cast<int>(a.offsets[e + 1]);
-        for (int p = p0; p < p1; p += 64, ++it) {
+      for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t)) {
+        const int m = t.m0 + rank * 128, j = t.j0 + rank * t.half;
+        for (int p = t.p0; p < t.p1; p += 64, ++it) {
           const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kHalf;
           ok = t5_wait(&b->empty[s], ((it / kStages) & 1) ^ 1);
           if (!ok) break;
-          const bool whole = p + 64 <= p1;
-          if (rank == 0) mbar_arrive_expect_tx(&b->full[s], whole ? 2 * (2 + (kGather ? 0 : half / 64)) * kBlock : 0);
+          const bool whole = p + 64 <= t.p1;
+          if (rank == 0) mbar_arrive_expect_tx(&b->full[s], whole ? 2 * (2 + (kGather ? 0 : t.half / 64)) * kBlock : 0);
           if (whole) {
             const u32 bar = leader_bar(&b->full[s]);
             tma_load_2d(sa, &map_p, m, p, bar);
             tma_load_2d(sa + kBlock, &map_p, m + 64, p, bar);
             if (!kGather) {
               tma_load_2d(sb, &map_x, j, p, bar);
-              if (half > 64) tma_load_2d(sb + kBlock, &map_x, j + 64, p, bar);
+              if (t.half > 64) tma_load_2d(sb + kBlock, &map_x, j + 64, p, bar);
             }
           }
         }
@@ -617,26 +683,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
     if (lane == 0 && rank == 0) {
       u32 it = 0, n_done = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-        const int e = static_cast<int>(id / n_per), j0 = static_cast<int>(id % n_per) / n_mt * kTileN;
-        const int p0 = static_cast<int>(a.offsets[e]), p1 = static_cast<int>(a.offsets[e + 1]);
-        if (p0 >= p1) continue;
-        const u32 idesc = t5_idesc(a.type, true, true, kTileM, a.n_j - j0 > 128 ? 256 : 128), buf = n_done & 1, d = tmem + buf * kTileN;
+      for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t), ++n_done) {
+        const u32 idesc = t5_idesc(a.type, true, true, kTileM, 2 * t.half), buf = n_done & 1, d = tmem + buf * kTileN;
         ok = t5_wait(&b->sums_empty[buf], ((n_done >> 1) & 1) ^ 1);
         if (!ok) break;
         t5_fence_after();
-        for (int p = p0; p < p1; p += 64, ++it) {
+        for (int p = t.p0; p < t.p1; p += 64, ++it) {
           const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kHalf;
           ok = t5_wait(&b->full[s], (it / kStages) & 1);
           if (!ok) break;
           t5_fence_after();
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            t5_mma_f16(d, t5_desc_mn(sa + j * 16 * kRowBytes, kBlock), t5_desc_mn(sb + j * 16 * kRowBytes, kBlock), idesc, p > p0 || j > 0);
+            t5_mma_f16(d, t5_desc_mn(sa + j * 16 * kRowBytes, kBlock), t5_desc_mn(sb + j * 16 * kRowBytes, kBlock), idesc, p > t.p0 || j > 0);
           t5_commit(&b->empty[s]);
         }
         if (ok) t5_commit(&b->sums_full[buf]);
-        ++n_done;
       }
       if (!ok) {
         dev_set_error(a.err, kDevTimeout);
@@ -644,60 +706,55 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
       }
     }
     __syncwarp();
-  } else if (warp == 10) {
+  } else if (warp == 14) {
     if (lane == 0) {
       u32 it = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-        const int e = static_cast<int>(id / n_per), n_st = (static_cast<int>(a.offsets[e + 1] - a.offsets[e]) + 63) / 64;
-        for (int i = 0; ok && i < n_st; ++i, ++it) ok = hand_over(b, it);
-      }
+      for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t))
+        for (int p = t.p0; ok && p < t.p1; p += 64, ++it) ok = hand_over(b, it);
       if (!ok) dev_set_error(a.err, kDevTimeout);
     }
     __syncwarp();
   } else if (warp >= 6) {
-    // sixteen lanes have a row: 256 bytes of dP, 256 (or 128) of X
+    // sixteen lanes have a row: 256 bytes of dP, 256 (or 128) of X; a thread the rows r0 + 16 i of a stage
     const int thread = threadIdx.x - 192, c = thread & 15, r0 = thread >> 4;
-    const u32 at = (c >> 3) * kBlock + r0 * kRowBytes + (((c & 7) ^ r0) << 4);  // (rows r0 + 8 i: the same swizzle)
+    const u32 at = (c >> 3) * kBlock + r0 * kRowBytes + (((c & 7) ^ (r0 & 7)) << 4);  // (rows r0 + 16 i: the same swizzle)
     CopyQueue queue(b);
     bool ok = true;
-    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-      const int e = static_cast<int>(id / n_per), rest = static_cast<int>(id % n_per);
-      const int j0 = rest / n_mt * kTileN, half = a.n_j - j0 > 128 ? 128 : 64;
-      const int m = rest % n_mt * kTileM + rank * 128 + c * 8, j = j0 + rank * half + c * 8;
-      const int p0 = static_cast<int>(a.offsets[e]), p1 = static_cast<int>(a.offsets[e + 1]);
+    for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t)) {
+      const int m = t.m0 + rank * 128 + c * 8, j = t.j0 + rank * t.half + c * 8;
       const u32 m_bytes = 2 * max(0, min(8, a.n_m - m)), j_bytes = 2 * max(0, min(8, a.n_j - j));
       const char* dp = a.dp + (m_bytes ? 2 * static_cast<i64>(m) : 0);
       const char* x = a.x + (j_bytes ? 2 * static_cast<i64>(j) : 0);
-      int next[8], after[8];  // rows of X of the next stage and the one behind it
-      const auto rows_at = [&](int p, int (&to)[8]) {
+      int next[4], after[4];  // rows of X of the next stage and the one behind it
+      const auto rows_at = [&](int p, int (&to)[4]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int q = p + r0 + 8 * i;
-          to[i] = q < p1 ? (kGather ? a.rows[q] : q) : -1;
+        for (int i = 0; i < 4; ++i) {
+          const int q = p + r0 + 16 * i;
+          to[i] = q < t.p1 ? (kGather ? a.rows[q] : q) : -1;
         }
       };
-      rows_at(p0, next);
-      rows_at(p0 + 64, after);
-      for (int p = p0; p < p1; p += 64) {
+      rows_at(t.p0, next);
+      rows_at(t.p0 + 64, after);
+      for (int p = t.p0; p < t.p1; p += 64) {
         ok = queue.slot_free();
         if (!ok) break;
         const u32 dst = stage0 + queue.issued % kStages * kStage + at;
-        const bool whole = p + 64 <= p1;
-        if ((kGather || !whole) && c * 8 < half) {
+        const bool whole = p + 64 <= t.p1;
+        if ((kGather || !whole) && c * 8 < t.half) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            copy16(dst + kHalf + i * 8 * kRowBytes, next[i] >= 0 ? x + next[i] * a.x_stride : x, next[i] >= 0 ? j_bytes : 0);
+          for (int i = 0; i < 4; ++i)
+            copy16(dst + kHalf + i * 16 * kRowBytes, next[i] >= 0 ? x + next[i] * a.x_stride : x, next[i] >= 0 ? j_bytes : 0);
         }
         if (!whole) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int q = p + r0 + 8 * i;
-            copy16(dst + i * 8 * kRowBytes, q < p1 ? dp + q * a.dp_stride : dp, q < p1 ? m_bytes : 0);
+          for (int i = 0; i < 4; ++i) {
+            const int q = p + r0 + 16 * i;
+            copy16(dst + i * 16 * kRowBytes, q < t.p1 ? dp + q * a.dp_stride : dp, q < t.p1 ? m_bytes : 0);
           }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) next[i] = after[i];
+        for (int i = 0; i < 4; ++i) next[i] = after[i];
         rows_at(p + 128, after);
         queue.done();
       }
@@ -708,13 +765,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
     const int quad = warp & 3;
     u32 n_done = 0;
     bool ok = true;
-    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-      const int e = static_cast<int>(id / n_per), rest = static_cast<int>(id % n_per);
-      const int m = rest % n_mt * kTileM + rank * 128 + quad * 32 + lane, j0 = rest / n_mt * kTileN, n = min(kTileN, a.n_j - j0);
-      const bool some = a.offsets[e] < a.offsets[e + 1];
-      TO* out = static_cast<TO*>(a.out) + static_cast<i64>(e) * a.out_block + static_cast<i64>(m - lane) * a.out_stride + j0;
+    for (i64 id = blockIdx.x >> 1; ok && id < walk.n_tiles; id += gridDim.x >> 1) {
+      const DwTile t = walk.at(id);
+      const int e = static_cast<int>(id / walk.n_per), m = t.m0 + rank * 128 + quad * 32 + lane, n = min(kTileN, a.n_j - t.j0);
+      TO* out = static_cast<TO*>(a.out) + static_cast<i64>(e) * a.out_block + static_cast<i64>(m - lane) * a.out_stride + t.j0;
       const u32 buf = n_done & 1;
-      if (some) {
+      if (t.p0 < t.p1) {
         ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done >> 1) & 1));
         if (!ok) break;
         t5_fence_after();
@@ -724,6 +780,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
           t5_wait_ld();
           if (m < a.n_m) store_run(out + lane * a.out_stride + c, n - c, a.out_align, v);
         }
+        t5_fence_before();
+        if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
+        ++n_done;
       } else {  // a column without entries
         for (int r = 0; r < 32 && m - lane + r < a.n_m; ++r)
           if (a.out_align >= 16) {
@@ -734,11 +793,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(352, 1)
           } else {
             for (int c = lane; c < n; c += 32) out[r * a.out_stride + c] = from_float<TO>(0.f);
           }
-      }
-      if (some) {
-        t5_fence_before();
-        if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
-        ++n_done;
       }
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);

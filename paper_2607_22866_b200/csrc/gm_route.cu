@@ -542,7 +542,7 @@ int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dens
     a.type = dP->dtype == GM_BF16 ? 1 : 0;
     a.err = route->err;
     const i64 tiles = static_cast<i64>(a.E) * ((a.n_m + kTileM - 1) / kTileM) * ((a.n_j + kTileN - 1) / kTileN);
-    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 352, kT5Smem, st, map_p, map_x, a); };
+    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 480, kT5Smem + (a.E + 1) * 4, st, map_p, map_x, a); };
     switch (dW->dtype) {
       case GM_F32: return by_entry ? go.template operator()<k_route_dw<false, float>>() : go.template operator()<k_route_dw<true, float>>();
       case GM_BF16: return by_entry ? go.template operator()<k_route_dw<false, __nv_bfloat16>>() : go.template operator()<k_route_dw<true, __nv_bfloat16>>();
