@@ -528,7 +528,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
     for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
       const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
       const int m = static_cast<int>(id % n_mt) * kTileM + rank * 128 + quad * 32 + lane;
-      const int mine = t.n - half * 128;  // places of this warp's half of the columns
+      const int each = round32(t.n) / 2, mine = min(each, t.n - half * each);  // places of this warp's half of the columns
       u64 acc[64];                        // two places each
 #pragma unroll
       for (int j = 0; j < 64; ++j) acc[j] = 0;
@@ -538,8 +538,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
         ok = __all_sync(0xffffffffu, t5_wait(&sb->full[s], (it / kScaleSlots) & 1) && t5_wait(&b->sums_full[buf], (it >> 1) & 1));
         if (!ok) break;
         t5_fence_after();
-        const u32 from = tmem + buf * kTileN + half * 128 + (static_cast<u32>(quad * 32) << 16);
-        const float4* sx = reinterpret_cast<const float4*>(scales + s * kScaleSlot + half * 128);
+        const u32 from = tmem + buf * kTileN + half * each + (static_cast<u32>(quad * 32) << 16);
+        const float4* sx = reinterpret_cast<const float4*>(scales + s * kScaleSlot + half * each);
         u64 w2 = 0;
         if (kRowScales) {
           const u32 w = __float_as_uint(scales[s * kScaleSlot + kTileN + quad * 32 + lane]);
@@ -578,7 +578,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
 #pragma unroll
           for (int j = 0; j < 8; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(v[2 * j]), "=r"(v[2 * j + 1]) : "l"(acc[c * 8 + j]));
           if (c * 16 < mine)
-            store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + half * 128 + c * 16, mine - c * 16, m, a.n_m, v);
+            store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + half * each + c * 16, mine - c * 16, m, a.n_m, v);
         }
       }
     }
