@@ -22,11 +22,23 @@ namespace gm {
 
 constexpr int kTileM = 256;        // rows of a block of W (or of dW) per tile, half of them per block of threads
 constexpr int kTileN = 256;        // places (or columns of dW) per tile
+constexpr int kFewN = 64;          // the same where columns of R have few places
 constexpr int kRowBytes = 128;     // of one operand row in a stage: 64 values of 16 bits, 128 of 8
-constexpr int kStages = 6;
-constexpr int kHalf = 128 * kRowBytes;  // one block's share of an operand in a stage
-constexpr int kStage = 2 * kHalf;
+constexpr int kHalf = 128 * kRowBytes;  // one block's share of 256 rows of an operand in a stage
 constexpr u32 kTmemColumns = 512;
+constexpr int kMostStages = 10;
+
+// How a block's memory is used with kN places per tile.  Few places leave room for more stages, and tensor memory for more buffers:
+// then the weights alone bound the products, and what counts is how much of them is on its way.
+template <int kN>
+struct Shape {
+  static constexpr int kStages = kN == kTileN ? 6 : 10;
+  static constexpr int kStage = kHalf + kN / 2 * kRowBytes;
+  static constexpr int kBuffers = kTmemColumns / kN;  // of sums
+  static_assert(kStages <= kMostStages, "barriers");
+};
+constexpr int kStages = Shape<kTileN>::kStages, kStage = Shape<kTileN>::kStage;
+constexpr int kMostBuffers = Shape<kFewN>::kBuffers;
 
 struct ProductArgs {
   const i64* offsets;
@@ -37,6 +49,7 @@ struct ProductArgs {
   i64 x_stride;
   void* out;
   i64 out_stride;
+  int out_align;        // bytes that the rows' addresses are multiples of
   u32 type;             // of the operands in the instruction descriptor
   const float* xs;      // 8 bits: scales of X (rows x blocks of k) ...
   i64 xs_stride;
@@ -70,27 +83,28 @@ constexpr int kIndexSlot = 128;  // one block's rows of a tile
 
 // The barriers and the place in tensor memory of a block, behind its stages.
 struct T5Block {
-  u64 full[kStages], empty[kStages], copied[kStages];
-  u64 sums_full[2], sums_empty[2], drain;
+  u64 full[kMostStages], empty[kMostStages], copied[kMostStages];
+  u64 sums_full[kMostBuffers], sums_empty[kMostBuffers], drain;
   u32 tmem;
   u32 scan_tmp[34];
   int index[2 * kIndexSlot];
 };
 
-// Places of each column, cut into parts of at most kTileN places that differ by less than 32 in size.
+// Places of each column, cut into parts of at most kN places that differ by less than 32 in size.
 struct Part { int e, first, n; };
 __device__ __forceinline__ int round32(int n) { return (n + 31) & ~31; }
-__device__ __forceinline__ int part_count(int places) { return (places + kTileN - 1) / kTileN; }
+template <int kN> __device__ __forceinline__ int part_count(int places) { return (places + kN - 1) / kN; }
 __device__ __forceinline__ int part_size(int places, int parts) { return round32((places + parts - 1) / parts); }
 
 // off[e]: first place of column e; part[e]: parts of the columns before it.  All threads of the block.
+template <int kN>
 __device__ __forceinline__ void list_parts(const i64* __restrict__ offsets, int E, int* off, int* part, u32* scan_tmp) {
   u32 before = 0;
   for (int e0 = 0; e0 <= E; e0 += blockDim.x) {
     const int e = e0 + threadIdx.x;
     int a = 0, n = 0;
     if (e <= E) a = static_cast<int>(offsets[e]);
-    if (e < E) n = part_count(static_cast<int>(offsets[e + 1]) - a);
+    if (e < E) n = part_count<kN>(static_cast<int>(offsets[e + 1]) - a);
     u32 total;
     const u32 first = before + block_exclusive_scan(static_cast<u32>(n), scan_tmp, &total);
     before += total;
@@ -118,8 +132,8 @@ __device__ __forceinline__ char* t5_align(char* p) { return p + ((1024 - (smem_u
 __device__ __forceinline__ void t5_begin(T5Block* b, int full_arrivals, int result_warps, int copy_threads) {
   grid_launch_next();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&b->full[i], full_arrivals); mbar_init(&b->empty[i], 1); mbar_init(&b->copied[i], copy_threads); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&b->sums_full[i], 1); mbar_init(&b->sums_empty[i], 2 * result_warps); }
+    for (int i = 0; i < kMostStages; ++i) { mbar_init(&b->full[i], full_arrivals); mbar_init(&b->empty[i], 1); mbar_init(&b->copied[i], copy_threads); }
+    for (int i = 0; i < kMostBuffers; ++i) { mbar_init(&b->sums_full[i], 1); mbar_init(&b->sums_empty[i], 2 * result_warps); }
     mbar_init(&b->drain, 1);
     mbar_fence_init();
   }
@@ -139,6 +153,7 @@ __device__ __forceinline__ void t5_end(u32 tmem) {
   if (threadIdx.x < 32) tmem_free(tmem, kTmemColumns);
 }
 // After a wait that gave up: the copies in flight are waited for (with a limit) before the blocks leave.
+template <int kStages = gm::kStages>
 __device__ __forceinline__ void t5_drain_copies(T5Block* b, u32 issued) {
   for (u32 i = issued > kStages ? issued - kStages : 0; i < issued; ++i) t5_wait(&b->full[i % kStages], (i / kStages) & 1);
 }
@@ -150,6 +165,7 @@ __device__ __forceinline__ void t5_drain_matrix(T5Block* b) {
 // Rows by index: the copying threads go as far ahead as there are stages.  Their copies arrive on the stage's own barrier of the block;
 // one thread that has no copies under way itself makes them visible to the matrix instructions and tells the leader.  (A copying
 // thread's own fence waits for all its copies, the next stages' too: 43 us instead of 25 for a product of one row.)
+template <int kStages = gm::kStages>
 struct CopyQueue {
   T5Block* b;
   u32 issued = 0;
@@ -164,6 +180,7 @@ struct CopyQueue {
   }
 };
 
+template <int kStages = gm::kStages>
 __device__ __forceinline__ bool hand_over(T5Block* b, u32 stage) {
   if (!t5_wait(&b->copied[stage % kStages], (stage / kStages) & 1)) return false;
   fence_to_matrix();
@@ -172,21 +189,23 @@ __device__ __forceinline__ bool hand_over(T5Block* b, u32 stage) {
 }
 
 // The rows of X of one block's half of the places, for every tile and stage: eight lanes have a row of a stage.
-template <int kValueBytes>
+// kFixed: the first 128 of the tile's places (or the others), else half of them.
+template <int kN, int kValueBytes, bool kFixed>
 __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u32 stage0, int* index, const int* off, const int* part, i64 n_tiles,
                                             int n_mt, int thread) {
-  CopyQueue queue(b);
+  using S = Shape<kN>;
+  CopyQueue<S::kStages> queue(b);
   const int n_kb = (a.n_k * kValueBytes + kRowBytes - 1) / kRowBytes, c = thread & 7, r0 = thread >> 3, lane = thread & 31;
   const u32 at = kHalf + r0 * kRowBytes + ((c ^ (r0 & 7)) << 4);  // (rows r0 + 16 i: the same swizzle)
-  constexpr int kApart = 16, kRows = 8;  // a thread's rows: r0 + 16 i
+  constexpr int kApart = 16, kRows = kN / 2 / kApart;  // a thread's rows: r0 + 16 i
   const int my_row = (thread >> 5) * 4 + (lane & 3) + kApart * (lane >> 2);  // the one whose index this lane brings in for its warp
   const i64 width = static_cast<i64>(a.n_k) * kValueBytes;
   const u32 rank = cluster_rank();
   const i64 pairs = gridDim.x >> 1;
   const auto bring_rows = [&](i64 id, int slot) {
-    if (id >= n_tiles) return;
+    if (id >= n_tiles || lane >= 4 * kRows) return;
     const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-    const int half = round32(t.n) / 2, p = rank * half + my_row;
+    const int half = kFixed ? 128 : round32(t.n) / 2, p = rank * half + my_row;
     int* to = index + slot * kIndexSlot + my_row;
     if (my_row < half && p < t.n) copy4(smem_u32(to), a.rows + t.first + p);
     else *to = -1;
@@ -197,9 +216,9 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
   copy_commit();
   for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += pairs, slot ^= 1) {
     const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-    const int half = round32(t.n) / 2;
+    const int half = kFixed ? 128 : round32(t.n) / 2;
     // this tile's rows came with the last tile's first stage
-    if (n_kb > kStages && id >= pairs) copy_wait<kStages>();
+    if (n_kb > S::kStages && id >= pairs) copy_wait<S::kStages>();
     else copy_wait_all();
     __syncwarp();
     const char* src[kRows];
@@ -218,13 +237,13 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
     for (int kb = 0; kb < n_kb; ++kb) {
       ok = queue.slot_free();
       if (!ok) break;
-      const u32 dst = stage0 + queue.issued % kStages * kStage + at;
+      const u32 dst = stage0 + queue.issued % S::kStages * S::kStage + at;
       const i64 x = static_cast<i64>(kb) * kRowBytes + c * 16;
       const u32 bytes = static_cast<u32>(max(static_cast<i64>(0), min(static_cast<i64>(16), width - x)));
       const i64 from = bytes ? x : 0;
 #pragma unroll
       for (int i = 0; i < kRows; ++i)
-        if (r0 + kApart * i < half) copy16(dst + i * kApart * kRowBytes, src[i] + from, there >> i & 1 ? bytes : 0);
+        if (r0 + kApart * i < half && (!kFixed || (there >> i & 1))) copy16(dst + i * kApart * kRowBytes, src[i] + from, there >> i & 1 ? bytes : 0);
       queue.done();
     }
   }
@@ -232,17 +251,20 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
   if (!ok && (thread & 31) == 0) dev_set_error(a.err, kDevTimeout);
 }
 
+template <int kN>
 __device__ __forceinline__ void hand_over_rows(const ProductArgs& a, T5Block* b, i64 n_tiles, int n_kb) {
   const i64 pairs = gridDim.x >> 1, mine = (n_tiles - (blockIdx.x >> 1) + pairs - 1) / pairs * n_kb;
   bool ok = true;
-  for (i64 it = 0; ok && it < mine; ++it) ok = hand_over(b, static_cast<u32>(it));
+  for (i64 it = 0; ok && it < mine; ++it) ok = hand_over<Shape<kN>::kStages>(b, static_cast<u32>(it));
   if (!ok) dev_set_error(a.err, kDevTimeout);
 }
 
 // Tiles of W (and of X with a row per place) by tensor map.  One warp; lane 0 has W, lane i 32 rows of X.
-template <int kValueBytes, bool kAmn, bool kGather>
+template <int kN, int kValueBytes, bool kAmn, bool kGather, bool kFixed>
 __device__ __forceinline__ void copy_tiles(const ProductArgs& a, const CUtensorMap* map_w, const CUtensorMap* map_x, T5Block* b, u32 stage0,
                                            const int* off, const int* part, i64 n_tiles, int n_mt) {
+  using S = Shape<kN>;
+  constexpr int kStages = S::kStages, kStage = S::kStage;
   constexpr int kStep = kRowBytes / kValueBytes;
   const int lane = threadIdx.x & 31, n_kb = (a.n_k + kStep - 1) / kStep;
   const u32 rank = cluster_rank();
@@ -250,7 +272,7 @@ __device__ __forceinline__ void copy_tiles(const ProductArgs& a, const CUtensorM
   bool ok = true;
   for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
     const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-    const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128, half = round32(t.n) / 2;
+    const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128, half = kFixed ? 128 : round32(t.n) / 2;
     const u32 bytes = 2 * (kHalf + (kGather ? 0 : round32(half) * kRowBytes));
     for (int kb = 0; kb < n_kb; ++kb, ++it) {
       const u32 s = it % kStages, sa = stage0 + s * kStage;
@@ -271,7 +293,7 @@ __device__ __forceinline__ void copy_tiles(const ProductArgs& a, const CUtensorM
   }
   if (!ok) {
     if (lane == 0) dev_set_error(a.err, kDevTimeout);
-    if (rank == 0) t5_drain_copies(b, it);
+    if (rank == 0) t5_drain_copies<kStages>(b, it);
   }
 }
 
@@ -331,9 +353,11 @@ __device__ __forceinline__ void store_run(TO* __restrict__ out, int n, int align
 // kAmn: W is contiguous along its own rows m, not along k (the product with W itself instead of its transpose).
 // kGather: X has a row per row of R, fetched by index; else a row per place.
 // Warps: 0 copies by tensor map, 1 matrix instructions, 2-5 results, 6-9 copies by index, 10 hands those over.
-template <bool kAmn, bool kGather, typename TO>
+template <int kN, bool kAmn, bool kGather, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192, 1)
     k_route_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const ProductArgs a) {
+  using S = Shape<kN>;
+  constexpr int kStages = S::kStages, kStage = S::kStage, kBuffers = S::kBuffers;
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
   T5Block* b = reinterpret_cast<T5Block*>(stages + kStages * kStage);
@@ -343,22 +367,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
   const u32 rank = cluster_rank();
   t5_begin(b, kGather ? 3 : 1, 4, 128);
   grid_wait();
-  list_parts(a.offsets, a.E, off, part, b->scan_tmp);
+  list_parts<kN>(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 63) / 64;
   const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
   zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
 
   if (warp == 0) {
-    copy_tiles<2, kAmn, kGather>(a, &map_w, &map_x, b, stage0, off, part, n_tiles, n_mt);
+    copy_tiles<kN, 2, kAmn, kGather, false>(a, &map_w, &map_x, b, stage0, off, part, n_tiles, n_mt);
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       u32 it = 0, n_done = 0;
       bool ok = true;
       for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1, ++n_done) {
         const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-        const u32 idesc = t5_idesc(a.type, kAmn, false, kTileM, round32(t.n)), buf = n_done & 1, d = tmem + buf * kTileN;
-        ok = t5_wait(&b->sums_empty[buf], ((n_done >> 1) & 1) ^ 1);
+        const u32 idesc = t5_idesc(a.type, kAmn, false, kTileM, round32(t.n)), buf = n_done % kBuffers, d = tmem + buf * kN;
+        ok = t5_wait(&b->sums_empty[buf], ((n_done / kBuffers) & 1) ^ 1);
         if (!ok) break;
         t5_fence_after();
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
@@ -388,13 +412,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
     for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1, ++n_done) {
       const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
       const int m = static_cast<int>(id % n_mt) * kTileM + rank * 128 + quad * 32 + lane;
-      const u32 buf = n_done & 1;
-      ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done >> 1) & 1));
+      const u32 buf = n_done % kBuffers;
+      ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done / kBuffers) & 1));
       if (!ok) break;
       t5_fence_after();
       for (int c = 0; c < t.n; c += 16) {
         u32 v[16];
-        t5_ld16(v, tmem + buf * kTileN + c + (static_cast<u32>(quad * 32) << 16));
+        t5_ld16(v, tmem + buf * kN + c + (static_cast<u32>(quad * 32) << 16));
         t5_wait_ld16(v);
         store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + c, t.n - c, m, a.n_m, v);
       }
@@ -403,24 +427,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   } else if (warp < 10) {
-    gather_rows<2>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 192);
+    gather_rows<kN, 2, false>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 192);
   } else {
-    if (lane == 0) hand_over_rows(a, b, n_tiles, n_kb);
+    if (lane == 0) hand_over_rows<kN>(a, b, n_tiles, n_kb);
     __syncwarp();
   }
   t5_end(tmem);
 }
 
-// 8 bits.  The sums of 128 values of k go to a buffer of their own in tensor memory; eight warps take them out, multiply by both
-// scales and add them up in registers (a thread: one row of W, half the places of the tile).  The scales come through a ring in
-// shared memory, a slot per block of k: those of the tile's places, times W's where it has one for each 128 rows, or 128 of W's behind
-// them (kRowScales).
+// 8 bits.  The sums of 128 values of k go to a buffer of their own in tensor memory; eight warps take them out, multiply by both scales
+// and add them up in registers.  The scales come through a ring in shared memory, a slot per block of k.
+//
+// Here the places are the lanes (the instruction's M) and the rows of W the columns, so that a thread has one place: its scale times
+// that of the 128 rows of W is one number per thread and block of k, and the rows of the result are stored in whole runs.  (With the rows of W
+// as lanes a scale per column has to be read from shared memory for every sum: 547 us instead of 385 at 32768 x 4096 x 2048.)
+// What bounds it is the way of the sums out of tensor memory: about 1100 cycles per block of k and tile, of which the matrix
+// instructions need 512.
+// kRowScales: W has scales for each row and 128 values, which are read from shared memory, else for each 128 rows.
 // Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 3 scales, 4-11 results.  The results' registers
 // are what the others give up: 512 threads begin with 128 each (384 with 168).
 constexpr int kScaleSlots = 8;
-constexpr int kScaleLag = 4;               // slots whose copies may be under way
-constexpr int kScaleSlot = kTileN + 128;  // floats
+constexpr int kScaleSlot = 128 + kTileM;  // floats: of a block's places, of the rows of W (or two for 128 of them each)
 struct ScaleBlock { u64 full[kScaleSlots], empty[kScaleSlots]; };
+
+// Brings in the scales of `rows` (of X, per lane, -1: none) and of W.  One warp.
+template <int kPlaces, bool kRowScales>
+__device__ __forceinline__ void copy_scales(const ProductArgs& a, u32 to, const int (&row)[kPlaces / 32], const float* ws, int m0, int n_w, int kb) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < kPlaces / 32; ++i)
+    if (row[i] >= 0) copy4(to + (lane + 32 * i) * 4, a.xs + row[i] * a.xs_stride + kb);
+  to += kPlaces * 4;
+  if (kRowScales) {
+    for (int i = lane; i < n_w; i += 32)
+      if (m0 + i < a.n_m) copy4(to + i * 4, ws + static_cast<i64>(m0 + i) * a.ws_row + kb);
+  } else if (lane * 128 < n_w && m0 + lane * 128 < a.n_m) {
+    copy4(to + lane * 4, ws + static_cast<i64>(m0 / 128 + lane) * a.ws_row + kb);
+  }
+}
 
 template <bool kGather, bool kRowScales, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384, 1)
@@ -435,10 +479,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const u32 rank = cluster_rank();
   if (threadIdx.x == 32)
-    for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&sb->full[i], 1); mbar_init(&sb->empty[i], 8); }
+    for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&sb->full[i], 32); mbar_init(&sb->empty[i], 8); }
   t5_begin(b, kGather ? 3 : 1, 8, 128);
   grid_wait();
-  list_parts(a.offsets, a.E, off, part, b->scan_tmp);
+  list_parts<kTileN>(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 127) / 128;
   const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
   const u32 stage0 = smem_u32(stages), scale0 = smem_u32(scales), tmem = b->tmem;
@@ -447,20 +491,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kGather ? 48 : 88));
     if (warp == 0) {
-      copy_tiles<1, false, kGather>(a, &map_w, &map_x, b, stage0, off, part, n_tiles, n_mt);
+      copy_tiles<kTileN, 1, false, kGather, true>(a, &map_w, &map_x, b, stage0, off, part, n_tiles, n_mt);
     } else if (warp == 1 && lane == 0 && rank == 0) {
       u32 it = 0;
       bool ok = true;
+      const u32 idesc = t5_idesc(a.type, false, false, 256, 256);
       for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-        const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-        const u32 idesc = t5_idesc(a.type, false, false, kTileM, round32(t.n));
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
-          const u32 s = it % kStages, sa = stage0 + s * kStage, sx = sa + kHalf, buf = it & 1, d = tmem + buf * kTileN;
+          const u32 s = it % kStages, sw = stage0 + s * kStage, sx = sw + kHalf, buf = it & 1, d = tmem + buf * 256;
           ok = t5_wait(&b->sums_empty[buf], ((it >> 1) & 1) ^ 1) && t5_wait(&b->full[s], (it / kStages) & 1);
           if (!ok) break;
           t5_fence_after();
 #pragma unroll
-          for (int j = 0; j < 4; ++j) t5_mma_f8(d, t5_desc_k(sa + j * 32), t5_desc_k(sx + j * 32), idesc, j > 0);
+          for (int j = 0; j < 4; ++j) t5_mma_f8(d, t5_desc_k(sx + j * 32), t5_desc_k(sw + j * 32), idesc, j > 0);
           t5_commit(&b->empty[s]);
           t5_commit(&b->sums_full[buf]);
         }
@@ -470,66 +513,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
         t5_drain_matrix(b);
       }
     } else if (kGather && warp == 2 && lane == 0) {
-      hand_over_rows(a, b, n_tiles, n_kb);
+      hand_over_rows<kTileN>(a, b, n_tiles, n_kb);
     } else if (warp == 3) {
       u32 it = 0;
       bool ok = true;
-      const auto hand_scales = [&](u32 i) {  // a slot whose copies have arrived: each lane multiplies what it has copied itself
-        float* at = scales + i % kScaleSlots * kScaleSlot + lane;
-        if (!kRowScales) {
-          const float w = at[kTileN];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) at[32 * j] *= w;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sb->full[i % kScaleSlots]);
-      };
       for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
         const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-        const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128;
+        const int m0 = static_cast<int>(id % n_mt) * kTileM;
         const float* ws = a.ws + static_cast<i64>(t.e) * a.ws_block;
-        int row[8];
+        int row[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int p = lane + 32 * i;
+        for (int i = 0; i < 4; ++i) {
+          const int p = rank * 128 + lane + 32 * i;
           row[i] = p < t.n ? (kGather ? a.rows[t.first + p] : t.first + p) : -1;
         }
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
-          const u32 s = it % kScaleSlots, to = scale0 + (s * kScaleSlot + lane) * 4;
+          const u32 s = it % kScaleSlots;
           ok = __all_sync(0xffffffffu, t5_wait(&sb->empty[s], ((it / kScaleSlots) & 1) ^ 1));
           if (!ok) break;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (row[i] >= 0) copy4(to + 128 * i, a.xs + row[i] * a.xs_stride + kb);
-          if (kRowScales) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (m0 + lane + 32 * i < a.n_m) copy4(to + (kTileN + 32 * i) * 4, ws + static_cast<i64>(m0 + lane + 32 * i) * a.ws_row + kb);
-          } else {  // (every lane has its own copy of W's)
-            copy4(to + kTileN * 4, ws + static_cast<i64>(min(m0, a.n_m - 1) / 128) * a.ws_row + kb);
-          }
-          copy_commit();
-          if (it >= kScaleLag) {
-            copy_wait<kScaleLag>();
-            hand_scales(it - kScaleLag);
-          }
+          copy_scales<128, kRowScales>(a, scale0 + s * kScaleSlot * 4, row, ws, m0, kTileM, kb);
+          copy_arrive(&sb->full[s]);
         }
       }
       copy_wait_all();
-      for (u32 i = it > kScaleLag ? it - kScaleLag : 0; i < it; ++i) hand_scales(i);
       if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
     }
     __syncwarp();
   } else if (warp < 12) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(208));
-    const int quad = warp & 3, half = (warp - 4) >> 2;
+    const int quad = warp & 3, half = (warp - 4) >> 2, place = rank * 128 + quad * 32 + lane;
     u32 it = 0;
     bool ok = true;
     for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
       const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m = static_cast<int>(id % n_mt) * kTileM + rank * 128 + quad * 32 + lane;
-      const int each = round32(t.n) / 2, mine = min(each, t.n - half * each);  // places of this warp's half of the columns
-      u64 acc[64];                        // two places each
+      const int m = static_cast<int>(id % n_mt) * kTileM + half * 128;  // this warp's first row of W
+      const bool some = place - lane < t.n;                              // whether this warp has places at all
+      u64 acc[64];                                                       // two rows of W each
 #pragma unroll
       for (int j = 0; j < 64; ++j) acc[j] = 0;
 #pragma unroll 1
@@ -538,27 +557,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
         ok = __all_sync(0xffffffffu, t5_wait(&sb->full[s], (it / kScaleSlots) & 1) && t5_wait(&b->sums_full[buf], (it >> 1) & 1));
         if (!ok) break;
         t5_fence_after();
-        const u32 from = tmem + buf * kTileN + half * each + (static_cast<u32>(quad * 32) << 16);
-        const float4* sx = reinterpret_cast<const float4*>(scales + s * kScaleSlot + half * each);
-        u64 w2 = 0;
-        if (kRowScales) {
-          const u32 w = __float_as_uint(scales[s * kScaleSlot + kTileN + quad * 32 + lane]);
-          w2 = pair_of(w, w);
-        }
-        u32 v[2][16];
-        t5_ld16(v[0], from);
+        if (some) {
+          const float* slot = scales + s * kScaleSlot;
+          const float x = slot[quad * 32 + lane] * (kRowScales ? 1.f : slot[128 + half]);
+          const u64 x2 = pair_of(__float_as_uint(x), __float_as_uint(x));
+          const u32 from = tmem + buf * 256 + half * 128 + (static_cast<u32>(quad * 32) << 16);
+          const u32 sw = smem_u32(slot + 128 + half * 128);
+          u32 v[2][16];
+          t5_ld16(v[0], from);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {  // sixteen places: the next ones are on their way while these are added up
-          if (c * 16 < mine || c == 0) {
-            u64 x[8];
+          for (int c = 0; c < 8; ++c) {  // sixteen rows of W: the next ones are on their way while these are added up
+            u64 w[8];
+            if (kRowScales) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float4 f = sx[c * 4 + j];
-              x[2 * j] = pair_of(__float_as_uint(f.x), __float_as_uint(f.y));
-              x[2 * j + 1] = pair_of(__float_as_uint(f.z), __float_as_uint(f.w));
+              for (int j = 0; j < 4; ++j)
+                asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(w[2 * j]), "=l"(w[2 * j + 1]) : "r"(sw + (c * 16 + j * 4) * 4));
             }
             t5_wait_ld16(v[c & 1]);
-            if (c + 1 < 8 && (c + 1) * 16 < mine) {
+            if (c + 1 < 8) {
               t5_ld16(v[(c + 1) & 1], from + (c + 1) * 16);
             } else {  // all out: the buffer is free
               t5_fence_before();
@@ -566,17 +582,151 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-              fma2(acc[c * 8 + j], pair_of(v[c & 1][2 * j], v[c & 1][2 * j + 1]), kRowScales ? mul2(x[j], w2) : x[j]);
+              fma2(acc[c * 8 + j], pair_of(v[c & 1][2 * j], v[c & 1][2 * j + 1]), kRowScales ? mul2(w[j], x2) : x2);
           }
+        } else {
+          t5_fence_before();
+          if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
         }
         if (lane == 0) mbar_arrive(&sb->empty[s]);
       }
+      if (ok && place < t.n) {
+        TO* out = static_cast<TO*>(a.out) + (static_cast<i64>(t.first) + place) * a.out_stride + m;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          u32 v[32];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(v[2 * j]), "=r"(v[2 * j + 1]) : "l"(acc[c * 16 + j]));
+          if (m + c * 32 < a.n_m) store_run(out + c * 32, a.n_m - m - c * 32, a.out_align, v);
+        }
+      }
+    }
+    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(48));
+    gather_rows<kTileN, 1, true>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 384);
+  }
+  t5_end(tmem);
+}
+
+// The same for columns of R with few places: they are the columns again (the instruction's N, 32 or 64), eight buffers of sums and ten stages
+// keep W on its way, and a thread has one row of W and up to 32 places, whose scales it reads from shared memory.
+// Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 3 scales, 4-11 results.
+constexpr int kFewSlot = kFewN + 128;
+template <bool kGather, bool kRowScales, typename TO>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384, 1)
+    k_route_product_scaled_few(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const ProductArgs a) {
+  using S = Shape<kFewN>;
+  constexpr int kStages = S::kStages, kStage = S::kStage, kBuffers = S::kBuffers;
+  extern __shared__ char t5_sm[];
+  char* stages = t5_align(t5_sm);
+  float* scales = reinterpret_cast<float*>(stages + kStages * kStage);
+  T5Block* b = reinterpret_cast<T5Block*>(scales + kScaleSlots * kFewSlot);
+  ScaleBlock* sb = reinterpret_cast<ScaleBlock*>(b + 1);
+  int* off = reinterpret_cast<int*>(sb + 1);
+  int* part = off + a.E + 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const u32 rank = cluster_rank();
+  if (threadIdx.x == 32)
+    for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&sb->full[i], 32); mbar_init(&sb->empty[i], 8); }
+  t5_begin(b, kGather ? 3 : 1, 8, 128);
+  grid_wait();
+  list_parts<kFewN>(a.offsets, a.E, off, part, b->scan_tmp);
+  const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 127) / 128;
+  const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
+  const u32 stage0 = smem_u32(stages), scale0 = smem_u32(scales), tmem = b->tmem;
+  zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
+
+  if (warp == 0) {
+    copy_tiles<kFewN, 1, false, kGather, false>(a, &map_w, &map_x, b, stage0, off, part, n_tiles, n_mt);
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      u32 it = 0;
+      bool ok = true;
+      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+        const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+        const u32 idesc = t5_idesc(a.type, false, false, kTileM, round32(t.n));
+        for (int kb = 0; kb < n_kb; ++kb, ++it) {
+          const u32 s = it % kStages, sw = stage0 + s * kStage, sx = sw + kHalf, buf = it % kBuffers, d = tmem + buf * kFewN;
+          ok = t5_wait(&b->sums_empty[buf], ((it / kBuffers) & 1) ^ 1) && t5_wait(&b->full[s], (it / kStages) & 1);
+          if (!ok) break;
+          t5_fence_after();
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t5_mma_f8(d, t5_desc_k(sw + j * 32), t5_desc_k(sx + j * 32), idesc, j > 0);
+          t5_commit(&b->empty[s]);
+          t5_commit(&b->sums_full[buf]);
+        }
+      }
+      if (!ok) {
+        dev_set_error(a.err, kDevTimeout);
+        t5_drain_matrix(b);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    if (kGather && lane == 0) hand_over_rows<kFewN>(a, b, n_tiles, n_kb);
+    __syncwarp();
+  } else if (warp == 3) {
+    u32 it = 0;
+    bool ok = true;
+    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+      const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+      const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128;
+      const float* ws = a.ws + static_cast<i64>(t.e) * a.ws_block;
+      int row[kFewN / 32];
+#pragma unroll
+      for (int i = 0; i < kFewN / 32; ++i) {
+        const int p = lane + 32 * i;
+        row[i] = p < t.n ? (kGather ? a.rows[t.first + p] : t.first + p) : -1;
+      }
+      for (int kb = 0; kb < n_kb; ++kb, ++it) {
+        const u32 s = it % kScaleSlots;
+        ok = __all_sync(0xffffffffu, t5_wait(&sb->empty[s], ((it / kScaleSlots) & 1) ^ 1));
+        if (!ok) break;
+        copy_scales<kFewN, kRowScales>(a, scale0 + s * kFewSlot * 4, row, ws, m0, 128, kb);
+        copy_arrive(&sb->full[s]);
+      }
+    }
+    copy_wait_all();
+    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+  } else if (warp < 12) {
+    const int quad = warp & 3, half = (warp - 4) >> 2;
+    u32 it = 0;
+    bool ok = true;
+    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+      const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+      const int m = static_cast<int>(id % n_mt) * kTileM + rank * 128 + quad * 32 + lane;
+      const int each = round32(t.n) / 2, mine = min(each, t.n - half * each);  // places of this warp's half of the columns
+      float acc[2][16] = {};
+#pragma unroll 1
+      for (int kb = 0; kb < n_kb; ++kb, ++it) {
+        const u32 buf = it % kBuffers, s = it % kScaleSlots;
+        ok = __all_sync(0xffffffffu, t5_wait(&sb->full[s], (it / kScaleSlots) & 1) && t5_wait(&b->sums_full[buf], (it / kBuffers) & 1));
+        if (!ok) break;
+        t5_fence_after();
+        const float* slot = scales + s * kFewSlot;
+        const float w = slot[kFewN + (kRowScales ? quad * 32 + lane : 0)];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          if (c * 16 < mine) {
+            u32 v[16];
+            t5_ld16(v, tmem + buf * kFewN + half * each + c * 16 + (static_cast<u32>(quad * 32) << 16));
+            t5_wait_ld16(v);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[c][j] = fmaf(__uint_as_float(v[j]), slot[half * each + c * 16 + j] * w, acc[c][j]);
+          }
+        t5_fence_before();
+        if (lane == 0) {
+          mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
+          mbar_arrive(&sb->empty[s]);
+        }
+      }
       if (ok) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
+        for (int c = 0; c < 2; ++c) {
           u32 v[16];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(v[2 * j]), "=r"(v[2 * j + 1]) : "l"(acc[c * 8 + j]));
+          for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(acc[c][j]);
           if (c * 16 < mine)
             store_places(static_cast<TO*>(a.out), a.out_stride, static_cast<i64>(t.first) + half * each + c * 16, mine - c * 16, m, a.n_m, v);
         }
@@ -584,8 +734,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(48));
-    gather_rows<1>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 384);
+    gather_rows<kFewN, 1, false>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 384);
   }
   t5_end(tmem);
 }
@@ -711,7 +860,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
       u32 it = 0;
       bool ok = true;
       for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t))
-        for (int p = t.p0; ok && p < t.p1; p += 64, ++it) ok = hand_over(b, it);
+        for (int p = t.p0; ok && p < t.p1; p += 64, ++it) ok = hand_over<>(b, it);
       if (!ok) dev_set_error(a.err, kDevTimeout);
     }
     __syncwarp();
@@ -719,7 +868,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
     // sixteen lanes have a row: 256 bytes of dP, 256 (or 128) of X; a thread the rows r0 + 16 i of a stage
     const int thread = threadIdx.x - 192, c = thread & 15, r0 = thread >> 4;
     const u32 at = (c >> 3) * kBlock + r0 * kRowBytes + (((c & 7) ^ (r0 & 7)) << 4);  // (rows r0 + 16 i: the same swizzle)
-    CopyQueue queue(b);
+    CopyQueue<> queue(b);
     bool ok = true;
     for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t)) {
       const int m = t.m0 + rank * 128 + c * 8, j = t.j0 + rank * t.half + c * 8;

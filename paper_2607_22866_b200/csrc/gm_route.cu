@@ -78,6 +78,13 @@ static int check_out(const gm_dense* M, const char* name) {
     return fail(GM_ERR_INVALID_ARG, std::string(name) + ": rows of a result overlap");
   return GM_OK;
 }
+// The largest power of two, up to 32, that the addresses of a result's rows are multiples of.
+static int out_align(const gm_dense& M) {
+  const i64 es = static_cast<i64>(elem_size(M.dtype));
+  int align = 32;
+  while (align > 1 && (reinterpret_cast<uintptr_t>(M.data) % align || (M.n_rows > 1 && M.row_stride * es % align) || (M.n_blocks > 1 && M.block_stride * es % align))) align /= 2;
+  return align;
+}
 static int check_shape(const gm_dense* M, const char* name, i64 blocks, i64 rows, i64 cols) {
   if (M->n_blocks != blocks || M->n_rows != rows || M->n_cols != cols)
     return fail(GM_ERR_DIM_MISMATCH, std::string(name) + ": " + std::to_string(M->n_blocks) + " x " + std::to_string(M->n_rows) + " x " + std::to_string(M->n_cols) +
@@ -204,12 +211,20 @@ static int allow_most_smem() {
   return GM_OK;
 }
 
-constexpr size_t kT5Smem = static_cast<size_t>(kStages) * kStage + 1024 + sizeof(T5Block);
-constexpr size_t kScaleSmem = kScaleSlots * kScaleSlot * 4 + sizeof(ScaleBlock);
+template <int kN>
+constexpr size_t kT5Smem = static_cast<size_t>(Shape<kN>::kStages) * Shape<kN>::kStage + 1024 + sizeof(T5Block);
+template <int kN>
+constexpr size_t kScaleSmem = kScaleSlots * (kN == kFewN ? kFewSlot : kScaleSlot) * 4 + sizeof(ScaleBlock);
+template <int kN>
 static size_t product_smem(int E, bool bits8) {
-  return kT5Smem + static_cast<size_t>(E + 1) * 8 + (bits8 ? kScaleSmem : 0);
+  return kT5Smem<kN> + static_cast<size_t>(E + 1) * 8 + (bits8 ? kScaleSmem<kN> : 0);
 }
-static_assert(kT5Smem + (kRouteMaxCols + 1) * 8 + kScaleSmem <= kMostSmem, "fits a block's shared memory");
+static_assert(std::max(kT5Smem<kTileN> + kScaleSmem<kTileN>, kT5Smem<kFewN> + kScaleSmem<kFewN>) + (kRouteMaxCols + 1) * 8 <= kMostSmem, "fits a block's shared memory");
+
+// Whether tiles of few places are the better ones: as long as a column has at most half of such a tile's on average (the tiles of
+// 256 places then hold little, and give the weights fewer stages and buffers).
+static bool few_places(const gm_route* r) { return r->nnz <= static_cast<i64>(kFewN / 2) * std::min<i64>(r->E, r->nnz); }
+static i64 tile_count(const gm_route* r, i64 n_m, int n) { return ((r->nnz + n - 1) / n + std::min<i64>(r->E, r->nnz)) * ((n_m + kTileM - 1) / kTileM); }
 
 // Whether clusters of kRouteBlocks fit the current device (more than 8 blocks are not promised), found out once.
 static bool wide_clusters() {
@@ -310,13 +325,16 @@ static int product(const gm_route* r, const gm_dense& X, bool by_entry, const gm
   a.out_stride = out.row_stride;
   a.type = X.dtype == GM_BF16 ? 1 : 0;
   a.err = r->err;
-  const i64 tiles = ((r->nnz + kTileN - 1) / kTileN + std::min<i64>(r->E, r->nnz)) * ((n_m + kTileM - 1) / kTileM);
-  const size_t smem = product_smem(r->E, false);
-  const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, by_entry ? 192 : 352, smem, st, map_w, map_x, a); };
   const auto typed = [&](auto* tag) {
     using TO = std::remove_pointer_t<decltype(tag)>;
-    if (m_inner) return by_entry ? go.template operator()<k_route_product<true, false, TO>>() : go.template operator()<k_route_product<true, true, TO>>();
-    return by_entry ? go.template operator()<k_route_product<false, false, TO>>() : go.template operator()<k_route_product<false, true, TO>>();
+    const auto sized = [&]<int kN>() {
+      const auto go = [&]<auto kernel>() {
+        return launch_t5<kernel>(tile_count(r, n_m, kN), num_sms, by_entry ? 192 : 352, product_smem<kN>(r->E, false), st, map_w, map_x, a);
+      };
+      if (m_inner) return by_entry ? go.template operator()<k_route_product<kN, true, false, TO>>() : go.template operator()<k_route_product<kN, true, true, TO>>();
+      return by_entry ? go.template operator()<k_route_product<kN, false, false, TO>>() : go.template operator()<k_route_product<kN, false, true, TO>>();
+    };
+    return few_places(r) ? sized.template operator()<kFewN>() : sized.template operator()<kTileN>();
   };
   switch (out.dtype) {
     case GM_F32: return typed(static_cast<float*>(nullptr));
@@ -535,14 +553,11 @@ int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dens
     a.out = dW->data;
     a.out_block = dW->block_stride;
     a.out_stride = dW->row_stride;
-    const i64 oes = static_cast<i64>(elem_size(dW->dtype));
-    for (a.out_align = 32; a.out_align > 8; a.out_align /= 2)
-      if (reinterpret_cast<uintptr_t>(dW->data) % a.out_align == 0 && (dW->n_rows <= 1 || dW->row_stride * oes % a.out_align == 0) &&
-          (dW->n_blocks <= 1 || dW->block_stride * oes % a.out_align == 0)) break;
+    a.out_align = out_align(*dW);
     a.type = dP->dtype == GM_BF16 ? 1 : 0;
     a.err = route->err;
     const i64 tiles = static_cast<i64>(a.E) * ((a.n_m + kTileM - 1) / kTileM) * ((a.n_j + kTileN - 1) / kTileN);
-    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 480, kT5Smem + (a.E + 1) * 4, st, map_p, map_x, a); };
+    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 480, kT5Smem<kTileN> + (a.E + 1) * 4, st, map_p, map_x, a); };
     switch (dW->dtype) {
       case GM_F32: return by_entry ? go.template operator()<k_route_dw<false, float>>() : go.template operator()<k_route_dw<true, float>>();
       case GM_BF16: return by_entry ? go.template operator()<k_route_dw<false, __nv_bfloat16>>() : go.template operator()<k_route_dw<true, __nv_bfloat16>>();
@@ -706,6 +721,7 @@ int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_
     a.places = route->nnz;
     a.out = P->data;
     a.out_stride = P->row_stride;
+    a.out_align = out_align(*P);
     a.type = 0;
     a.xs = static_cast<const float*>(xs.data);
     a.xs_stride = xs.row_stride;
@@ -713,13 +729,17 @@ int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_
     a.ws_block = ws.block_stride;
     a.ws_row = ws.row_stride;
     a.err = route->err;
-    const i64 tiles = ((route->nnz + kTileN - 1) / kTileN + std::min<i64>(route->E, route->nnz)) * ((a.n_m + kTileM - 1) / kTileM);
-    const size_t smem = product_smem(route->E, true);
-    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, by_entry ? 384 : 512, smem, st, map_w, map_x, a); };
+    const bool few = few_places(route);
+    const i64 tiles = tile_count(route, a.n_m, few ? kFewN : kTileN);
+    const size_t smem = few ? product_smem<kFewN>(route->E, true) : product_smem<kTileN>(route->E, true);
     const auto typed = [&](auto* tag) {
       using TO = std::remove_pointer_t<decltype(tag)>;
-      if (row_scales) return by_entry ? go.template operator()<k_route_product_scaled<false, true, TO>>() : go.template operator()<k_route_product_scaled<true, true, TO>>();
-      return by_entry ? go.template operator()<k_route_product_scaled<false, false, TO>>() : go.template operator()<k_route_product_scaled<true, false, TO>>();
+      const auto go = [&]<bool kGather, bool kRowScales>() {
+        const auto with = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, by_entry ? 384 : 512, smem, st, map_w, map_x, a); };
+        return few ? with.template operator()<k_route_product_scaled_few<kGather, kRowScales, TO>>() : with.template operator()<k_route_product_scaled<kGather, kRowScales, TO>>();
+      };
+      if (row_scales) return by_entry ? go.template operator()<false, true>() : go.template operator()<true, true>();
+      return by_entry ? go.template operator()<false, false>() : go.template operator()<true, false>();
     };
     switch (P->dtype) {
       case GM_F32: return typed(static_cast<float*>(nullptr));
