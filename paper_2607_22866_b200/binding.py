@@ -369,11 +369,13 @@ def _dims(t: torch.Tensor, where: str, name: str, dims: int):
         raise GmError(-2, where, f"{name}: {t.dim()} dimensions instead of {dims}")
 
 
-def _is_here(where: str, device: torch.device, stream) -> bool:
-    """Whether the call can run as it is: on the current device, on its current stream."""
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
+_current_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+
+
+def _on_cuda(where: str, device: torch.device):
     if device.type != "cuda":
         raise GmError(-1, where, f"tensors on {device}: a CUDA device expected")
-    return stream is None and device.index == torch._C._cuda_getDevice()
 
 
 def _there(call, device: torch.device, stream, *args, **kwargs):
@@ -397,6 +399,7 @@ class Route:
     def __init__(self, handle, R: DeviceCSR, stream: int, memory: torch.Tensor):
         self._h, self.R, self._stream, self._memory = handle, R, stream, memory
         self.n_rows, self.n_cols, self.nnz, self.device = R.n_rows, R.n_cols, R.nnz, memory.device
+        self._index = self.device.index
 
     def _places(self, k: int) -> torch.Tensor:
         first = 2 * (self.n_cols + 1) + k * self.nnz
@@ -423,7 +426,7 @@ class Route:
         _check(load_library().gm_route_status(self._h), "gm_route_status")
 
     def _current_stream(self) -> int:
-        stream = torch._C._cuda_getCurrentRawStream(self.device.index)
+        stream = _current_raw_stream(self._index)
         if stream != self._stream:  # not the one its memory belongs to
             s = torch.cuda.current_stream(self.device)
             for t in (self._memory, self.R.row_ptr, self.R.val):
@@ -447,7 +450,8 @@ def route_plan(R: DeviceCSR, stream=None) -> Route:
     column is outside [0, R.n_cols) is routed nowhere."""
     where = "gm_route_plan"
     device = R.row_ptr.device
-    if not _is_here(where, device, stream):
+    _on_cuda(where, device)
+    if stream is not None or device.index != _current_device():
         for t in (R.row_ptr, R.col, R.val):
             if stream is not None and t.is_cuda:
                 t.record_stream(stream)
@@ -458,7 +462,7 @@ def route_plan(R: DeviceCSR, stream=None) -> Route:
         raise GmError(-1, where, "R's arrays are shorter than its sizes say")
     n_off = 2 * (R.n_cols + 1)
     memory = torch.empty(n_off + 3 * R.nnz, dtype=torch.int32, device=device)
-    st, h, at = torch._C._cuda_getCurrentRawStream(device.index), ctypes.c_void_p(), memory.data_ptr()
+    st, h, at = _current_raw_stream(device.index), ctypes.c_void_p(), memory.data_ptr()
     rows = at + 4 * n_off
     _check(load_library().gm_route_plan(_byref(R._struct()), at, rows, rows + 4 * R.nnz, rows + 8 * R.nnz, st, _byref(h)), where)
     return Route(h, R, st, memory)
@@ -468,7 +472,7 @@ def route_product(route: Route, X: torch.Tensor, W: torch.Tensor, by_entry: bool
     """gm_route_product: P[p] = X[row of place p] @ W[its column].T, (nnz, N), in `dtype` (default: X's).  X (n_rows, K), or with
     by_entry (nnz, K) with a row for each place; W (n_cols, N, K); bf16 or f16."""
     where, device = "gm_route_product", route.device
-    if not _is_here(where, device, stream):
+    if stream is not None or route._index != _current_device():
         return _there(route_product, device, stream, route, X, W, by_entry, dtype)
     _dims(X, where, "X", 2)
     _dims(W, where, "W", 3)
@@ -482,7 +486,7 @@ def route_product(route: Route, X: torch.Tensor, W: torch.Tensor, by_entry: bool
 def route_product_dx(route: Route, dP: torch.Tensor, W: torch.Tensor, by_entry: bool = False, dtype=None, stream=None) -> torch.Tensor:
     """gm_route_product_dx: the gradient of route_product with respect to X, (n_rows, K), or (nnz, K) with by_entry."""
     where, device = "gm_route_product_dx", route.device
-    if not _is_here(where, device, stream):
+    if stream is not None or route._index != _current_device():
         return _there(route_product_dx, device, stream, route, dP, W, by_entry, dtype)
     _dims(dP, where, "dP", 2)
     _dims(W, where, "W", 3)
@@ -496,7 +500,7 @@ def route_product_dx(route: Route, dP: torch.Tensor, W: torch.Tensor, by_entry: 
 def route_product_dw(route: Route, dP: torch.Tensor, X: torch.Tensor, by_entry: bool = False, dtype=None, stream=None) -> torch.Tensor:
     """gm_route_product_dw: the gradient of route_product with respect to W, (n_cols, N, K)."""
     where, device = "gm_route_product_dw", route.device
-    if not _is_here(where, device, stream):
+    if stream is not None or route._index != _current_device():
         return _there(route_product_dw, device, stream, route, dP, X, by_entry, dtype)
     _dims(dP, where, "dP", 2)
     _dims(X, where, "X", 2)
@@ -509,7 +513,7 @@ def route_product_dw(route: Route, dP: torch.Tensor, X: torch.Tensor, by_entry: 
 def route_sum(route: Route, P: torch.Tensor, weighted: bool = True, dtype=None, stream=None) -> torch.Tensor:
     """gm_route_sum: Y[i] = sum over the entries of row i of R of their row of P, times R's value if `weighted`.  P (nnz, N) by place."""
     where, device = "gm_route_sum", route.device
-    if not _is_here(where, device, stream):
+    if stream is not None or route._index != _current_device():
         return _there(route_sum, device, stream, route, P, weighted, dtype)
     _dims(P, where, "P", 2)
     Y = _empty(P, route.n_rows, P.shape[1], dtype)
@@ -520,7 +524,7 @@ def route_sum(route: Route, P: torch.Tensor, weighted: bool = True, dtype=None, 
 def route_sum_grads(route: Route, dY: torch.Tensor, P: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
     """gm_route_sum_grads: gradients of the weighted route_sum, dP (nnz, N) by place and dval (nnz,) float32 by entry of R."""
     where, device = "gm_route_sum_grads", route.device
-    if not _is_here(where, device, stream):
+    if stream is not None or route._index != _current_device():
         return _there(route_sum_grads, device, stream, route, dY, P)
     _dims(dY, where, "dY", 2)
     _dims(P, where, "P", 2)
@@ -535,7 +539,8 @@ def block_quantize(X: torch.Tensor, block_rows: int = 1, stream=None) -> tuple[t
     """gm_block_quantize: (values in float8_e4m3fn, float32 scales) of X (rows, K) or (blocks, rows, K), bf16 or f16, with a scale for
     each block of block_rows (1 or 128) x 128."""
     where, device = "gm_block_quantize", X.device
-    if not _is_here(where, device, stream):
+    _on_cuda(where, device)
+    if stream is not None or device.index != _current_device():
         return _there(block_quantize, device, stream, X, block_rows)
     if block_rows not in (1, 128):
         raise GmError(-1, where, "block_rows: 1 or 128 expected")
@@ -545,7 +550,7 @@ def block_quantize(X: torch.Tensor, block_rows: int = 1, stream=None) -> tuple[t
     Q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
     S = torch.empty((*shape[:-2], -(-shape[-2] // block_rows), -(-shape[-1] // 128)), dtype=torch.float32, device=device)
     _check(load_library().gm_block_quantize(_dense(X, where, device), block_rows, _dense(Q, where, device),
-                                            _dense(S, where, device), torch._C._cuda_getCurrentRawStream(device.index)), where)
+                                            _dense(S, where, device), _current_raw_stream(device.index)), where)
     return Q, S
 
 
@@ -554,7 +559,7 @@ def route_product_scaled(route: Route, Xq: torch.Tensor, Xs: torch.Tensor, Wq: t
     """gm_route_product_scaled: route_product of float8_e4m3fn factors with scales, as block_quantize gives them: Xs (rows of X, K / 128),
     Ws (n_cols, N / 128, K / 128) or (n_cols, N, K / 128), all rounded up."""
     where, device = "gm_route_product_scaled", route.device
-    if not _is_here(where, device, stream):
+    if stream is not None or route._index != _current_device():
         return _there(route_product_scaled, device, stream, route, Xq, Xs, Wq, Ws, by_entry, dtype)
     for t, name, dims in ((Xq, "Xq", 2), (Xs, "Xs", 2), (Wq, "Wq", 3), (Ws, "Ws", 3)):
         _dims(t, where, name, dims)

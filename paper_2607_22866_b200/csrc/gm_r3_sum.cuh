@@ -59,12 +59,7 @@ template <> struct Vec8<__half> {
   }
 };
 
-// kVec: rows are 16-byte aligned and a multiple of eight wide; a thread then has eight columns, else one.
-template <typename T, bool kVec>
-__device__ __forceinline__ void load_cols(const T* p, float (&v)[8]) {
-  if (kVec) Vec8<T>::load(p, v);
-  else v[0] = static_cast<float>(*p);
-}
+// kVec: rows are 16-byte aligned and a multiple of eight wide; a thread then has 16 bytes of columns at a time, else one column.
 template <typename T, bool kVec>
 __device__ __forceinline__ void store_cols(T* p, const float (&v)[8]) {
   if (kVec) Vec8<T>::store(p, v);
@@ -172,7 +167,6 @@ __global__ void __launch_bounds__(kSumThreads) k_route_sum(const SumArgs a, int 
 // A warp per entry, in the order of the rows of R (so that a row's entries share its row of dY in cache).
 template <typename T, typename TD, bool kVec>
 __global__ void __launch_bounds__(256) k_route_sum_grads(const SumArgs a, TD* __restrict__ dp, i64 dp_stride, float* __restrict__ dval) {
-  constexpr int kCols = kVec ? 8 : 1;
   const int lane = threadIdx.x & 31;
   const i64 q = static_cast<i64>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
   grid_launch_next();
@@ -181,25 +175,39 @@ __global__ void __launch_bounds__(256) k_route_sum_grads(const SumArgs a, TD* __
   const int at = a.pos[q];
   TD* out = dp + at * dp_stride;
   if (at >= a.offsets[a.E]) {  // routed nowhere
-    const float zero[8] = {};
-    for (int c = lane * kCols; c < a.width; c += 32 * kCols) store_cols<TD, kVec>(out + c, zero);
+    for (int c = lane; c < a.width; c += 32) out[c] = from_float<TD>(0.f);
     if (lane == 0) dval[q] = 0.f;
     return;
   }
   const float r = a.val[q];
   const T* dy = static_cast<const T*>(a.y) + a.rows[at] * a.y_stride;
   const T* p = static_cast<const T*>(a.p) + at * a.p_stride;
+  // four runs of columns of both rows in flight (110 us without, 96 us with them, at 44231 x 2880)
+  using R = Raw<T, kVec>;
+  constexpr int kCols = kVec ? 16 / sizeof(T) : 1, kStep = 32 * kCols, kRuns = 4;
   float dot = 0.f;
-  for (int c = lane * kCols; c < a.width; c += 32 * kCols) {
-    float g[8], v[8];
-    load_cols<T, kVec>(dy + c, g);
-    load_cols<T, kVec>(p + c, v);
+  for (int c = lane * kCols; c < a.width; c += kStep * kRuns) {
+    typename R::type graw[kRuns], vraw[kRuns];
 #pragma unroll
-    for (int x = 0; x < kCols; ++x) {
-      dot = fmaf(g[x], v[x], dot);
-      g[x] *= r;
-    }
-    store_cols<TD, kVec>(out + c, g);
+    for (int u = 0; u < kRuns; ++u)
+      if (c + u * kStep < a.width) {
+        graw[u] = *reinterpret_cast<const typename R::type*>(dy + c + u * kStep);  // (other entries of the row read it too)
+        vraw[u] = R::load(p + c + u * kStep);
+      }
+#pragma unroll
+    for (int u = 0; u < kRuns; ++u)
+      if (c + u * kStep < a.width) {
+        float g[8], v[8];
+        R::values(graw[u], g);
+        R::values(vraw[u], v);
+#pragma unroll
+        for (int x = 0; x < kCols; ++x) {
+          dot = fmaf(g[x], v[x], dot);
+          g[x] *= r;
+        }
+        if constexpr (kCols == 4) store4(out + c + u * kStep, g);
+        else store_cols<TD, kVec>(out + c + u * kStep, g);
+      }
   }
   dot = warp_sum(dot);
   if (lane == 0) dval[q] = dot;
