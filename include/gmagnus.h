@@ -313,9 +313,9 @@ int gm_row_products_noalloc(const gm_csr* A, const gm_csr* B, int64_t* ip_out_de
  *
  * None of these calls waits for the device.  Work is enqueued on `cuda_stream`; scratch memory comes from the
  * allocator hook and goes back to it, with that stream, before the call returns.  They can be captured into a
- * CUDA graph once each kind has been called outside of a capture on the device; with a hook that
- * serves captures (or the default pool).  Sums are kept in 32 bits, in an order that depends on the shapes
- * and on R's structure only: the same call gives the same bits.
+ * CUDA graph, with a hook that serves captures (or the default pool); what they borrow has to live as long as the graph.
+ * Sums are kept in 32 bits, in an order that depends on the shapes and on R's structure only: the same call gives the
+ * same bits.  No call here records anything for automatic differentiation: gradients have calls of their own.
  * ------------------------------------------------------------------------------------------- */
 
 /* A dense array in device memory: n_blocks matrices of n_rows x n_cols, element strides (not negative; 0 repeats).

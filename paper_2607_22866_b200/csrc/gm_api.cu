@@ -104,6 +104,13 @@ constexpr int kMaxDevices = 64;
 static std::mutex g_facts_mutex;
 static DeviceFacts g_facts[kMaxDevices];
 
+// What the library looks up or allocates once for itself has nothing to do with a capture that this thread may have under way.
+struct OutsideCapture {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+  ~OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+
 static int device_facts(DeviceFacts* out) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) {
@@ -114,6 +121,7 @@ static int device_facts(DeviceFacts* out) {
   std::lock_guard<std::mutex> lock(g_facts_mutex);
   DeviceFacts& f = g_facts[dev];
   if (!f.known) {
+    OutsideCapture now;
     int n_dev = 0;
     if (cudaGetDeviceCount(&n_dev) != cudaSuccess || n_dev == 0) {
       cudaGetLastError();
@@ -191,6 +199,7 @@ static HostSlot* take_slot() {
   std::lock_guard<std::mutex> lock(g_slot_mutex);
   if (g_free_slots.empty()) {
     constexpr int kSlab = 64;
+    OutsideCapture now;
     void* slab = nullptr;
     if (cudaHostAlloc(&slab, kSlab * kHostSlotBytes, cudaHostAllocPortable | cudaHostAllocMapped) != cudaSuccess) {
       cudaGetLastError();

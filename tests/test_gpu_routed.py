@@ -4,6 +4,10 @@ Tolerances.  A result of type T is rounded once: at most eps_T / 2 of its size. 
 addition is off by at most one unit of the last place of a partial sum (a matrix unit may cut off instead of rounding), so by at
 most n * 2^-23 * sum |terms| altogether.  f16 results below its smallest normal number are off by at most half its smallest step, 2^-25.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -12,6 +16,7 @@ import paper_2607_22866_b200 as gm
 
 pytestmark = pytest.mark.gpu
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
 
 
@@ -515,6 +520,95 @@ def test_values_may_change_between_calls():
     gm.route_sum(route, P)
     R.val.mul_(2)
     assert torch.equal(gm.route_sum(route, P), gm.route_sum(gm.route_plan(R), P))
+
+
+@pytest.mark.parametrize("k", [1, 5])
+def test_many_columns(k):
+    # the most columns there may be, with tiles of few places (k = 1) and of many (k = 5: 75000 entries)
+    n, E, N, K = 30000, 2048, 24, 72
+    R = make_route(n, E, k, 21, drop=0.02)
+    route = gm.route_plan(R)
+    X, W = randn((n, K), BF16, 1), randn((E, N, K), BF16, 2)
+    ref, mag = product_reference(R, X, W, False)
+    close(gm.route_product(route, X, W, dtype=F32), ref, mag, K)
+    for rows in (1, 128):
+        (Xq, Xs), (Wq, Ws) = gm.block_quantize(X), gm.block_quantize(W, rows)
+        x, w = Xq.double() * Xs.double(), Wq.double() * Ws.double().repeat_interleave(rows, 1)[:, :N]
+        ref, mag = product_reference(R, x, w, False)
+        close(gm.route_product_scaled(route, Xq, Xs, Wq, Ws, dtype=F32), ref, mag, K + 3)
+    dP = randn((R.nnz, N), BF16, 3)
+    ref, mag, most = dw_reference(R, dP, X, False)
+    close(gm.route_product_dw(route, dP, X, dtype=F32), ref, mag, most)
+    torch.cuda.synchronize()
+    route.status()
+
+
+def test_offsets_beyond_32_bits():
+    # rows of P, X, dP and dW whose elements' numbers pass 2^31 (and whose bytes pass 2^32)
+    n, E, N, K = 70000, 3, 32776, 16
+    R = make_route(n, E, 1, 4)
+    route = gm.route_plan(R)
+    X, W = randn((n, K), BF16, 1), randn((E, N, K), BF16, 2)
+    P = gm.route_product(route, X, W)
+    assert P.numel() > 2**31
+    row, key, order, offsets, pos = reference_route(R)
+    places = np.r_[0:3, n // 2: n // 2 + 3, n - 300: n]
+    some = torch.from_numpy(places).cuda()
+    x, e = X[torch.from_numpy(row[order[places]]).cuda()].double(), torch.from_numpy(key[order[places]]).cuda()
+    ref = torch.einsum("pk,pnk->pn", x, W[e].double())
+    mag = torch.einsum("pk,pnk->pn", x.abs(), W[e].double().abs())
+    close(P[some], ref, mag, K)
+    # the sums over one entry each are the rows themselves, times a weight
+    Y = gm.route_sum(route, P)
+    last = torch.arange(n - 300, n, device="cuda")
+    rows = route.pos.long()[last]
+    ref = R.val.double()[last, None] * P[rows].double()
+    close(Y[last], ref, ref.abs(), 1)
+    dP, dval = gm.route_sum_grads(route, Y, P)
+    ref = Y[last].double() * P[rows].double()
+    close(dval[last], ref.sum(1), ref.abs().sum(1), N)
+    ref = R.val.double()[last, None] * Y[last].double()
+    close(dP[rows], ref, ref.abs(), 1)
+    dX = gm.route_product_dx(route, P, W)
+    at = torch.arange(n - 50, n, device="cuda")
+    e, p = torch.from_numpy(key).cuda()[at], P[route.pos.long()[at]].double()
+    close(dX[at], torch.einsum("pn,pnk->pk", p, W[e].double()), torch.einsum("pn,pnk->pk", p.abs(), W[e].double().abs()), N + 1)
+    dW = gm.route_product_dw(route, P, X)
+    a, b = int(offsets[2]), int(offsets[3])
+    x, g = X[torch.from_numpy(row[order[a:b]]).cuda()].double(), P[a:b, -64:].double()
+    close(dW[2, -64:], g.T @ x, g.abs().T @ x.abs(), b - a)
+    by_place = gm.route_product(route, P[:, :4096], randn((E, 24, 4096), BF16, 5), by_entry=True)  # rows 65552 bytes apart
+    again = gm.route_product(route, P[:, :4096].contiguous(), randn((E, 24, 4096), BF16, 5), by_entry=True)
+    assert torch.equal(by_place, again)
+
+
+def test_first_calls_of_a_process_in_a_capture():
+    # what the library looks up once for itself does not end a capture; 70 routes at a time need more than one slab of its host memory
+    code = """
+import torch, paper_2607_22866_b200 as gm
+n, E, N, K = 40, 3, 24, 64
+rp = torch.arange(n + 1, device="cuda")
+R = gm.DeviceCSR(n, E, rp, torch.arange(n, device="cuda", dtype=torch.int32) % E, torch.ones(n, device="cuda"))
+X, W = torch.ones(n, K, device="cuda").bfloat16(), torch.ones(E, N, K, device="cuda").bfloat16()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+routes = []
+with torch.cuda.graph(g):
+    for _ in range(70):
+        routes.append(gm.route_plan(R))
+    P = gm.route_product(routes[-1], X, W)
+    Y = gm.route_sum(routes[-1], P)
+    dX = gm.route_product_dx(routes[-1], P, W)
+    dW = gm.route_product_dw(routes[-1], P, X)
+    Q, S = gm.block_quantize(X)
+for t in (P, Y, dX, dW):
+    t.zero_()
+g.replay()
+torch.cuda.synchronize()
+assert (P == K).all() and (Y == K).all() and (dX == K * N).all() and dW[0, 0, 0] == K * 14, (P, Y, dX, dW)
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
 
 
 def refused(status, call):
