@@ -114,10 +114,16 @@ __global__ void __launch_bounds__(kRouteThreads, 1) k_route_plan(const i64* __re
     const int e = e0 + threadIdx.x;
     u32 all = 0, mine = 0;
     if (e < bins) {
-      for (unsigned b = 0; b < gridDim.x; ++b) {
-        const u32 v = cluster.map_shared_rank(sum, b)[e];
-        if (b < blockIdx.x) mine += v;
-        all += v;
+      for (unsigned b0 = 0; b0 < gridDim.x; b0 += 4) {  // (1, 2 or a multiple of four blocks)
+        u32 v[4];
+#pragma unroll
+        for (unsigned i = 0; i < 4; ++i) v[i] = cluster.map_shared_rank(sum, min(b0 + i, gridDim.x - 1))[e];
+#pragma unroll
+        for (unsigned i = 0; i < 4; ++i)
+          if (b0 + i < gridDim.x) {
+            if (b0 + i < blockIdx.x) mine += v[i];
+            all += v[i];
+          }
       }
     }
     u32 total;
