@@ -351,9 +351,10 @@ void gm_route_destroy(gm_route* route);
  * f16.  X: n_rows x K, a row for each row of R, or with by_entry nnz x K, a row for each place (what an earlier product gave). */
 int gm_route_product(const gm_route* route, const gm_dense* X, int by_entry, const gm_dense* W, const gm_dense* P, void* cuda_stream);
 /* Gradients of gm_route_product.  dX: with by_entry dP[p,:] * W[column] for each place, else that summed over the entries of
- * each row of R (in 32 bits, through nnz x K floats of scratch memory).  dW[e] = sum over the places p of column e of
+ * each row of R, in 32 bits, through scratch memory for the terms: `terms`, of nnz x K (rounded up to a multiple of 8) floats, aligned to
+ * 16 bytes, or NULL to let the call allocate it.  dW[e] = sum over the places p of column e of
  * dP[p,:]^T * X[row(p),:]; blocks of columns without entries are zero.  Results: f32, bf16 or f16. */
-int gm_route_product_dx(const gm_route* route, const gm_dense* dP, const gm_dense* W, int by_entry, const gm_dense* dX, void* cuda_stream);
+int gm_route_product_dx(const gm_route* route, const gm_dense* dP, const gm_dense* W, int by_entry, const gm_dense* dX, void* terms, void* cuda_stream);
 int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dense* X, int by_entry, const gm_dense* dW, void* cuda_stream);
 
 /* Y (n_rows x N) = for each row of R the sum of its entries' rows of P, times the entries' values if `weighted`.  Rows without

@@ -139,7 +139,7 @@ def load_library(install_torch_allocator: bool = True):
         lib.gm_route_destroy.argtypes = [vp]
         lib.gm_route_destroy.restype = None
         lib.gm_route_product.argtypes = [vp, D, ctypes.c_int, D, D, vp]
-        lib.gm_route_product_dx.argtypes = [vp, D, D, ctypes.c_int, D, vp]
+        lib.gm_route_product_dx.argtypes = [vp, D, D, ctypes.c_int, D, vp, vp]
         lib.gm_route_product_dw.argtypes = [vp, D, D, ctypes.c_int, D, vp]
         lib.gm_route_sum.argtypes = [vp, D, ctypes.c_int, D, vp]
         lib.gm_route_sum_grads.argtypes = [vp, D, D, D, vp, vp]
@@ -492,8 +492,9 @@ def route_product_dx(route: Route, dP: torch.Tensor, W: torch.Tensor, by_entry: 
     _dims(W, where, "W", 3)
     rows, K = route.nnz if by_entry else route.n_rows, W.shape[2]
     dX = _empty(dP, rows, K, dtype)
-    _check(load_library().gm_route_product_dx(route._h, _dense(dP, where, device), _dense(W, where, device), by_entry,
-                                              _result(dX, rows, K), route._current_stream()), where)
+    terms = None if by_entry else torch.empty(route.nnz * (K + 7 & ~7), dtype=torch.float32, device=device)
+    _check(load_library().gm_route_product_dx(route._h, _dense(dP, where, device), _dense(W, where, device), by_entry, _result(dX, rows, K),
+                                              terms.data_ptr() if terms is not None else None, route._current_stream()), where)
     return dX
 
 
@@ -547,10 +548,15 @@ def block_quantize(X: torch.Tensor, block_rows: int = 1, stream=None) -> tuple[t
     shape = X.shape
     if len(shape) not in (2, 3):
         raise GmError(-2, where, f"X: {len(shape)} dimensions instead of 2 or 3")
-    Q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
-    S = torch.empty((*shape[:-2], -(-shape[-2] // block_rows), -(-shape[-1] // 128)), dtype=torch.float32, device=device)
-    _check(load_library().gm_block_quantize(_dense(X, where, device), block_rows, _dense(Q, where, device),
-                                            _dense(S, where, device), _current_raw_stream(device.index)), where)
+    rows, cols = shape[-2], shape[-1]
+    s_rows, s_cols = -(-rows // block_rows), -(-cols // 128)
+    blocks = shape[0] if len(shape) == 3 else 1
+    Q = X.new_empty(shape, dtype=torch.float8_e4m3fn)
+    S = X.new_empty((s_rows, s_cols) if len(shape) == 2 else (blocks, s_rows, s_cols), dtype=torch.float32)
+    _check(load_library().gm_block_quantize(_dense(X, where, device), block_rows,
+                                            _pack_dense(Q.data_ptr(), blocks, rows, cols, rows * cols, cols, 1, 4, 0),
+                                            _pack_dense(S.data_ptr(), blocks, s_rows, s_cols, s_rows * s_cols, s_cols, 1, 0, 0),
+                                            _current_raw_stream(device.index)), where)
     return Q, S
 
 

@@ -317,36 +317,74 @@ __device__ __forceinline__ void store_places(TO* __restrict__ out, i64 stride, i
   }
 }
 
-// 32 consecutive values of a row, of which n are stored; `align`: bytes that every such address is a multiple of (32, 16, less).
+// 32 sums as results, two to a word where these have 16 bits.
 template <typename TO>
-__device__ __forceinline__ void store_run(TO* __restrict__ out, int n, int align, const u32 (&v)[32]) {
-  if (align >= 16 && n >= 32) {
-    constexpr int kWords = 32 * sizeof(TO) / 4;
-    u32 w[kWords];
-    if constexpr (sizeof(TO) == 4) {
+__device__ __forceinline__ void result_words(const u32 (&v)[32], u32 (&w)[8 * sizeof(TO)]) {
+  if constexpr (sizeof(TO) == 4) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) w[j] = v[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const TO lo = from_float<TO>(__uint_as_float(v[2 * j])), hi = from_float<TO>(__uint_as_float(v[2 * j + 1]));
-        w[j] = static_cast<u32>(*reinterpret_cast<const uint16_t*>(&lo)) | (static_cast<u32>(*reinterpret_cast<const uint16_t*>(&hi)) << 16);
-      }
-    }
-    if (align >= 32) {  // whole sectors of 32 bytes
-#pragma unroll
-      for (int j = 0; j < kWords; j += 8)
-        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(reinterpret_cast<u32*>(out) + j), "r"(w[j]), "r"(w[j + 1]), "r"(w[j + 2]),
-                     "r"(w[j + 3]), "r"(w[j + 4]), "r"(w[j + 5]), "r"(w[j + 6]), "r"(w[j + 7])
-                     : "memory");
-    } else {
-#pragma unroll
-      for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(reinterpret_cast<u32*>(out) + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
-    }
+    for (int j = 0; j < 32; ++j) w[j] = v[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j < n) out[j] = from_float<TO>(__uint_as_float(v[j]));
+    for (int j = 0; j < 16; ++j) {
+      const TO lo = from_float<TO>(__uint_as_float(v[2 * j])), hi = from_float<TO>(__uint_as_float(v[2 * j + 1]));
+      w[j] = static_cast<u32>(*reinterpret_cast<const uint16_t*>(&lo)) | (static_cast<u32>(*reinterpret_cast<const uint16_t*>(&hi)) << 16);
+    }
+  }
+}
+// 32 consecutive results at an address that is a multiple of `align` bytes, 16 at least.
+template <typename TO>
+__device__ __forceinline__ void store_run(TO* __restrict__ out, int align, const u32 (&v)[32]) {
+  constexpr int kWords = 8 * sizeof(TO);
+  u32 w[kWords];
+  result_words<TO>(v, w);
+  u32* to = reinterpret_cast<u32*>(out);
+  if (align >= 32) {  // whole sectors of 32 bytes
+#pragma unroll
+    for (int j = 0; j < kWords; j += 8)
+      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to + j), "r"(w[j]), "r"(w[j + 1]), "r"(w[j + 2]), "r"(w[j + 3]),
+                   "r"(w[j + 4]), "r"(w[j + 5]), "r"(w[j + 6]), "r"(w[j + 7])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(to + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+  }
+}
+// A warp's rows (a lane each) by up to 32 consecutive results, rows that start anywhere: sixteen words of sixteen rows change places among sixteen
+// lanes, then half a warp stores 64 consecutive bytes of a row (a lane's own row would be a sector per value: 100 us instead of 44 for 2631
+// rows of 1829 values).  All lanes call.
+template <typename TO>
+__device__ __forceinline__ void store_turned(TO* __restrict__ out, i64 stride, int rows, int n, int align, const u32 (&v)[32]) {
+  constexpr int kWords = 8 * sizeof(TO), kPer = 4 / sizeof(TO);  // values in a word
+  const int lane = threadIdx.x & 31;
+  u32 w[kWords];
+  result_words<TO>(v, w);
+#pragma unroll
+  for (int set = 0; set < kWords; set += 16) {
+#pragma unroll
+    for (int s = 8; s > 0; s >>= 1)
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if ((j & s) == 0) {
+          const bool upper = lane & s;
+          const u32 got = __shfl_xor_sync(0xffffffffu, upper ? w[set + j] : w[set + j + s], s);
+          if (upper) w[set + j] = got; else w[set + j + s] = got;
+        }
+    const int c = (set + (lane & 15)) * kPer;
+    TO* to = out + (lane & 16) * stride + c;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if ((lane & 16) + j < rows && c < n) {
+        if constexpr (kPer == 1) {
+          *reinterpret_cast<u32*>(to) = w[set + j];
+        } else if (align >= 4 && c + 1 < n) {
+          *reinterpret_cast<u32*>(to) = w[set + j];
+        } else {
+          *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(w[set + j]);
+          if (c + 1 < n) *reinterpret_cast<uint16_t*>(to + 1) = static_cast<uint16_t>(w[set + j] >> 16);
+        }
+      }
+      to += stride;
+    }
   }
 }
 
@@ -445,7 +483,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
 // instructions need 512.
 // kRowScales: W has scales for each row and 128 values, which are read from shared memory, else for each 128 rows.
 // Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 3 scales, 4-11 results.  The results' registers
-// are what the others give up: 512 threads begin with 128 each (384 with 168).
+// are what the others give up: 512 threads begin with 128 each.
 constexpr int kScaleSlots = 8;
 constexpr int kScaleSlot = 128 + kTileM;  // floats: of a block's places, of the rows of W (or two for 128 of them each)
 struct ScaleBlock { u64 full[kScaleSlots], empty[kScaleSlots]; };
@@ -467,7 +505,7 @@ __device__ __forceinline__ void copy_scales(const ProductArgs& a, u32 to, const 
 }
 
 template <bool kGather, bool kRowScales, typename TO>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
     k_route_product_scaled(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const ProductArgs a) {
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
@@ -489,7 +527,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
   zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kGather ? 48 : 88));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(48));
     if (warp == 0) {
       copy_tiles<kTileN, 1, false, kGather, true>(a, &map_w, &map_x, b, stage0, off, part, n_tiles, n_mt);
     } else if (warp == 1 && lane == 0 && rank == 0) {
@@ -590,21 +628,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
         }
         if (lane == 0) mbar_arrive(&sb->empty[s]);
       }
-      if (ok && place < t.n) {
-        TO* out = static_cast<TO*>(a.out) + (static_cast<i64>(t.first) + place) * a.out_stride + m;
+      if (ok && some) {
+        TO* out = static_cast<TO*>(a.out) + (static_cast<i64>(t.first) + place - lane) * a.out_stride + m;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           u32 v[32];
 #pragma unroll
           for (int j = 0; j < 16; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(v[2 * j]), "=r"(v[2 * j + 1]) : "l"(acc[c * 16 + j]));
-          if (m + c * 32 < a.n_m) store_run(out + c * 32, a.n_m - m - c * 32, a.out_align, v);
+          if (a.out_align >= 16 && a.n_m - m - c * 32 >= 32) {
+            if (place < t.n) store_run(out + lane * a.out_stride + c * 32, a.out_align, v);
+          } else if (m + c * 32 < a.n_m) {
+            store_turned(out + c * 32, a.out_stride, t.n - (place - lane), a.n_m - m - c * 32, a.out_align, v);
+          }
         }
       }
     }
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(48));
-    gather_rows<kTileN, 1, true>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 384);
+    if (kGather) gather_rows<kTileN, 1, true>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 384);
   }
   t5_end(tmem);
 }
@@ -927,7 +969,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
           u32 v[32];
           t5_ld32(v, tmem + buf * kTileN + c + (static_cast<u32>(quad * 32) << 16));
           t5_wait_ld();
-          if (m < a.n_m) store_run(out + lane * a.out_stride + c, n - c, a.out_align, v);
+          if (a.out_align >= 16 && n - c >= 32) {
+            if (m < a.n_m) store_run(out + lane * a.out_stride + c, a.out_align, v);
+          } else {
+            store_turned(out + c, a.out_stride, a.n_m - (m - lane), n - c, a.out_align, v);
+          }
         }
         t5_fence_before();
         if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
@@ -950,7 +996,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
   t5_end(tmem);
 }
 
-// Copies into an aligned layout: dst (blocks x rows x padded columns), the padding zero.
+// Copies rows of whole units (of 1 to 8 bytes) into rows that start on 16 bytes, the padding zero.  A warp has a row, four units of a lane in flight.
+template <typename T>
+__global__ void __launch_bounds__(256) k_route_pack_rows(const T* __restrict__ src, i64 block_stride, i64 row_stride, i64 n_blocks, i64 n_rows, int n_units,
+                                                         int padded, T* __restrict__ dst) {
+  const int lane = threadIdx.x & 31;
+  const i64 step = static_cast<i64>(gridDim.x) * 8;
+  grid_launch_next();
+  grid_wait();
+  for (i64 r = static_cast<i64>(blockIdx.x) * 8 + (threadIdx.x >> 5); r < n_blocks * n_rows; r += step) {
+    const i64 blk = r / n_rows;
+    const T* from = src + blk * block_stride + (r - blk * n_rows) * row_stride;
+    T* to = dst + r * padded;
+    for (int c = lane; c < padded; c += 128) {
+      T v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = c + 32 * i < n_units ? from[c + 32 * i] : T(0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + 32 * i < padded) to[c + 32 * i] = v[i];
+    }
+  }
+}
+
+// The same for any strides: dst (blocks x rows x padded columns).
 template <typename T>
 __global__ void k_route_pack(const T* __restrict__ src, i64 block_stride, i64 row_stride, i64 col_stride, i64 n_blocks, i64 n_rows,
                              i64 n_cols, i64 padded, T* __restrict__ dst) {

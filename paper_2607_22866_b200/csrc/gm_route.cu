@@ -148,13 +148,24 @@ static int pack(const gm_dense& M, Scratch* mem, int num_sms, gm_dense* out) {
   const size_t bytes = static_cast<size_t>(M.n_blocks) * M.n_rows * padded * es;
   void* p = mem->get(bytes);
   if (!p) return fail(GM_ERR_OOM, "no room for an aligned copy of " + std::to_string(bytes) + " bytes");
-  const i64 total = M.n_blocks * M.n_rows * padded;
-  const unsigned grid = static_cast<unsigned>(std::min<i64>((total + 255) / 256, static_cast<i64>(num_sms) * 16));
-  const auto go = [&](auto* tag) {
-    using T = std::remove_pointer_t<decltype(tag)>;
-    return launch(k_route_pack<T>, grid, 256, 0, mem->st, 0, static_cast<const T*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<T*>(p));
-  };
-  GM_TRY(es == 2 ? go(static_cast<uint16_t*>(nullptr)) : es == 4 ? go(static_cast<uint32_t*>(nullptr)) : go(static_cast<uint8_t*>(nullptr)));
+  if (M.col_stride == 1 || M.n_cols <= 1) {  // rows of whole units, as large as their addresses allow
+    i64 unit = 8;
+    while (unit > es && (reinterpret_cast<uintptr_t>(M.data) % unit || M.n_cols * es % unit || (M.n_rows > 1 && M.row_stride * es % unit) || (M.n_blocks > 1 && M.block_stride * es % unit))) unit /= 2;
+    const i64 grid = std::min<i64>((M.n_blocks * M.n_rows + 7) / 8, static_cast<i64>(num_sms) * 8);
+    const auto go = [&](auto* tag) {
+      using T = std::remove_pointer_t<decltype(tag)>;
+      return launch(k_route_pack_rows<T>, grid, 256, 0, mem->st, 0, static_cast<const T*>(M.data), M.block_stride * es / unit, M.row_stride * es / unit, M.n_blocks, M.n_rows,
+                    static_cast<int>(M.n_cols * es / unit), static_cast<int>(padded * es / unit), static_cast<T*>(p));
+    };
+    GM_TRY(unit == 8 ? go(static_cast<uint64_t*>(nullptr)) : unit == 4 ? go(static_cast<uint32_t*>(nullptr)) : unit == 2 ? go(static_cast<uint16_t*>(nullptr)) : go(static_cast<uint8_t*>(nullptr)));
+  } else {
+    const i64 grid = std::min<i64>((M.n_blocks * M.n_rows * padded + 255) / 256, static_cast<i64>(num_sms) * 16);
+    const auto go = [&](auto* tag) {
+      using T = std::remove_pointer_t<decltype(tag)>;
+      return launch(k_route_pack<T>, grid, 256, 0, mem->st, 0, static_cast<const T*>(M.data), M.block_stride, M.row_stride, M.col_stride, M.n_blocks, M.n_rows, M.n_cols, padded, static_cast<T*>(p));
+    };
+    GM_TRY(es == 2 ? go(static_cast<uint16_t*>(nullptr)) : es == 4 ? go(static_cast<uint32_t*>(nullptr)) : go(static_cast<uint8_t*>(nullptr)));
+  }
   *out = M;
   out->data = p;
   out->col_stride = 1;
@@ -371,8 +382,8 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
   const bool vec = rows_aligned(P) && rows_aligned(Y);
   // eight loads in flight per thread: of as many entries as rows have on average, and the rest of other columns
   const i64 mean = (r->nnz + r->n_rows - 1) / r->n_rows;
-  const int columns = !vec || mean > 4 ? 1 : mean > 2 ? 2 : 4;
-  const i64 per = kSumThreads * (vec ? columns * 16 / static_cast<i64>(elem_size(P.dtype)) : 1), chunks = (a.width + per - 1) / per;
+  const int columns = mean > 4 ? 1 : mean > 2 ? 2 : mean > 1 ? 4 : 8;
+  const i64 per = kSumThreads * columns * (vec ? 16 / static_cast<i64>(elem_size(P.dtype)) : 1), chunks = (a.width + per - 1) / per;
   GM_TRY(sum_grid(chunks * r->n_rows, "sum"));
   const auto go = [&](auto kernel) {
     return launch(kernel, chunks * r->n_rows, kSumThreads, 0, st, 0, a, static_cast<int>(chunks));
@@ -380,8 +391,10 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
   const auto typed2 = [&](auto* ti, auto* to) {
     using TI = std::remove_pointer_t<decltype(ti)>;
     using TO = std::remove_pointer_t<decltype(to)>;
-    if (!vec) return go(k_route_sum<TI, TO, false, 1>);
-    return columns == 1 ? go(k_route_sum<TI, TO, true, 1>) : columns == 2 ? go(k_route_sum<TI, TO, true, 2>) : go(k_route_sum<TI, TO, true, 4>);
+    const auto aligned = [&]<bool kVec>() {
+      return columns == 1 ? go(k_route_sum<TI, TO, kVec, 1>) : columns == 2 ? go(k_route_sum<TI, TO, kVec, 2>) : columns == 4 ? go(k_route_sum<TI, TO, kVec, 4>) : go(k_route_sum<TI, TO, kVec, 8>);
+    };
+    return vec ? aligned.template operator()<true>() : aligned.template operator()<false>();
   };
   const auto typed = [&](auto* ti) {
     switch (Y.dtype) {
@@ -486,7 +499,7 @@ int gm_route_product(const gm_route* route, const gm_dense* X, int by_entry, con
   });
 }
 
-int gm_route_product_dx(const gm_route* route, const gm_dense* dP, const gm_dense* W, int by_entry, const gm_dense* dX, void* cuda_stream) {
+int gm_route_product_dx(const gm_route* route, const gm_dense* dP, const gm_dense* W, int by_entry, const gm_dense* dX, void* terms, void* cuda_stream) {
   return guarded([&]() -> int {
     GM_TRY(route_ready(route));
     GM_TRY(check_dense(dP, "dP"));
@@ -508,7 +521,8 @@ int gm_route_product_dx(const gm_route* route, const gm_dense* dP, const gm_dens
     T.row_stride = (W->n_cols + 7) / 8 * 8;
     T.col_stride = 1;
     T.dtype = GM_F32;
-    T.data = mem.get(static_cast<size_t>(T.n_rows) * T.row_stride * 4);
+    if (reinterpret_cast<uintptr_t>(terms) % 16) return fail(GM_ERR_INVALID_ARG, "terms: not aligned to 16 bytes");
+    T.data = terms ? terms : mem.get(static_cast<size_t>(T.n_rows) * T.row_stride * 4);
     if (!T.data) return fail(GM_ERR_OOM, "no room for the entries' terms");
     GM_TRY(product(route, *dP, true, *W, true, T, st));
     return sum_rows(route, T, false, *dX, st);
@@ -735,7 +749,7 @@ int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_
     const auto typed = [&](auto* tag) {
       using TO = std::remove_pointer_t<decltype(tag)>;
       const auto go = [&]<bool kGather, bool kRowScales>() {
-        const auto with = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, by_entry ? 384 : 512, smem, st, map_w, map_x, a); };
+        const auto with = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, few && by_entry ? 384 : 512, smem, st, map_w, map_x, a); };
         return few ? with.template operator()<k_route_product_scaled_few<kGather, kRowScales, TO>>() : with.template operator()<k_route_product_scaled<kGather, kRowScales, TO>>();
       };
       if (row_scales) return by_entry ? go.template operator()<false, true>() : go.template operator()<true, true>();

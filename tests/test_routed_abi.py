@@ -53,7 +53,7 @@ def test_calls_without_a_route_are_refused(lib):
     m = dense(4, 8, BF16)
     assert lib.gm_route_status(None) == INVALID
     assert lib.gm_route_product(None, m, 0, m, m, None) == INVALID
-    assert lib.gm_route_product_dx(None, m, m, 0, m, None) == INVALID
+    assert lib.gm_route_product_dx(None, m, m, 0, m, None, None) == INVALID
     assert lib.gm_route_product_dw(None, m, m, 0, m, None) == INVALID
     assert lib.gm_route_sum(None, m, 1, m, None) == INVALID
     assert lib.gm_route_sum_grads(None, m, m, m, None, None) == INVALID
