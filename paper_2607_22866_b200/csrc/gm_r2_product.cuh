@@ -81,6 +81,17 @@ template <> __device__ __forceinline__ __half from_float<__half>(float v) { retu
 // Which rows of X a tile needs is itself copied into shared memory, during the tile before and by the warp that needs it.
 constexpr int kIndexSlot = 128;  // one block's rows of a tile
 
+// two values in a word, the first one in the low half
+template <typename T> __device__ __forceinline__ u32 pack_floats(float lo, float hi);
+template <> __device__ __forceinline__ u32 pack_floats<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const u32*>(&v);
+}
+template <> __device__ __forceinline__ u32 pack_floats<__half>(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const u32*>(&v);
+}
+
 // The barriers and the place in tensor memory of a block, behind its stages.
 struct T5Block {
   u64 full[kMostStages], empty[kMostStages], copied[kMostStages];
@@ -191,7 +202,7 @@ __device__ __forceinline__ bool hand_over(T5Block* b, u32 stage) {
 // The rows of X of one block's half of the places, for every tile and stage: eight lanes have a row of a stage.
 // kFixed: the first 128 of the tile's places (or the others), else half of them.
 template <int kN, int kValueBytes, bool kFixed>
-__device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u32 stage0, int* index, const int* off, const int* part, i64 n_tiles,
+__device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u32 stage0, int* index, const int* off, const int* part, u32 n_tiles,
                                             int n_mt, int thread) {
   using S = Shape<kN>;
   CopyQueue<S::kStages> queue(b);
@@ -201,10 +212,10 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
   const int my_row = (thread >> 5) * 4 + (lane & 3) + kApart * (lane >> 2);  // the one whose index this lane brings in for its warp
   const i64 width = static_cast<i64>(a.n_k) * kValueBytes;
   const u32 rank = cluster_rank();
-  const i64 pairs = gridDim.x >> 1;
-  const auto bring_rows = [&](i64 id, int slot) {
+  const u32 pairs = gridDim.x >> 1;
+  const auto bring_rows = [&](u32 id, int slot) {
     if (id >= n_tiles || lane >= 4 * kRows) return;
-    const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+    const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
     const int half = kFixed ? 128 : round32(t.n) / 2, p = rank * half + my_row;
     int* to = index + slot * kIndexSlot + my_row;
     if (my_row < half && p < t.n) copy4(smem_u32(to), a.rows + t.first + p);
@@ -214,8 +225,8 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
   int slot = 0;
   bring_rows(blockIdx.x >> 1, 0);
   copy_commit();
-  for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += pairs, slot ^= 1) {
-    const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+  for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += pairs, slot ^= 1) {
+    const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
     const int half = kFixed ? 128 : round32(t.n) / 2;
     // this tile's rows came with the last tile's first stage
     if (n_kb > S::kStages && id >= pairs) copy_wait<S::kStages>();
@@ -252,8 +263,8 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
 }
 
 template <int kN>
-__device__ __forceinline__ void hand_over_rows(const ProductArgs& a, T5Block* b, i64 n_tiles, int n_kb) {
-  const i64 pairs = gridDim.x >> 1, mine = (n_tiles - (blockIdx.x >> 1) + pairs - 1) / pairs * n_kb;
+__device__ __forceinline__ void hand_over_rows(const ProductArgs& a, T5Block* b, u32 n_tiles, int n_kb) {
+  const i64 pairs = gridDim.x >> 1, mine = (static_cast<i64>(n_tiles) - (blockIdx.x >> 1) + pairs - 1) / pairs * n_kb;
   bool ok = true;
   for (i64 it = 0; ok && it < mine; ++it) ok = hand_over<Shape<kN>::kStages>(b, static_cast<u32>(it));
   if (!ok) dev_set_error(a.err, kDevTimeout);
@@ -262,7 +273,7 @@ __device__ __forceinline__ void hand_over_rows(const ProductArgs& a, T5Block* b,
 // Tiles of W (and of X with a row per place) by tensor map.  One warp; lane 0 has W, lane i 32 rows of X.
 template <int kN, int kValueBytes, bool kAmn, bool kGather, bool kFixed>
 __device__ __forceinline__ void copy_tiles(const ProductArgs& a, const CUtensorMap* map_w, const CUtensorMap* map_x, T5Block* b, u32 stage0,
-                                           const int* off, const int* part, i64 n_tiles, int n_mt) {
+                                           const int* off, const int* part, u32 n_tiles, int n_mt) {
   using S = Shape<kN>;
   constexpr int kStages = S::kStages, kStage = S::kStage;
   constexpr int kStep = kRowBytes / kValueBytes;
@@ -270,9 +281,9 @@ __device__ __forceinline__ void copy_tiles(const ProductArgs& a, const CUtensorM
   const u32 rank = cluster_rank();
   u32 it = 0;
   bool ok = true;
-  for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-    const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-    const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128, half = kFixed ? 128 : round32(t.n) / 2;
+  for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+    const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
+    const int m0 = static_cast<int>(id % static_cast<u32>(n_mt)) * kTileM + rank * 128, half = kFixed ? 128 : round32(t.n) / 2;
     const u32 bytes = 2 * (kHalf + (kGather ? 0 : round32(half) * kRowBytes));
     for (int kb = 0; kb < n_kb; ++kb, ++it) {
       const u32 s = it % kStages, sa = stage0 + s * kStage;
@@ -325,10 +336,7 @@ __device__ __forceinline__ void result_words(const u32 (&v)[32], u32 (&w)[8 * si
     for (int j = 0; j < 32; ++j) w[j] = v[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const TO lo = from_float<TO>(__uint_as_float(v[2 * j])), hi = from_float<TO>(__uint_as_float(v[2 * j + 1]));
-      w[j] = static_cast<u32>(*reinterpret_cast<const uint16_t*>(&lo)) | (static_cast<u32>(*reinterpret_cast<const uint16_t*>(&hi)) << 16);
-    }
+    for (int j = 0; j < 16; ++j) w[j] = pack_floats<TO>(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
   }
 }
 // 32 consecutive results at an address that is a multiple of `align` bytes, 16 at least.
@@ -349,6 +357,23 @@ __device__ __forceinline__ void store_run(TO* __restrict__ out, int align, const
     for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(to + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
   }
 }
+// A warp's 32 rows (a lane each) by kOutRun results: laid down in shared memory (32 rows of 128 bytes, swizzled as the tensor map wants it), from
+// where one copy writes whole lines.  A lane's own row of 32 bytes per store took 3.3 us a tile of 256 x 256, more than a short sum's products.
+constexpr int kOutBytes = 32 * kRowBytes;
+template <typename TO> constexpr int kOutRun = kRowBytes / sizeof(TO);
+template <typename TO, int kFirst>  // 32 sums that are the values kFirst .. kFirst + 31 of the rows
+__device__ __forceinline__ void lay_down(u32 to, const u32 (&v)[32]) {
+  constexpr int kWords = 8 * sizeof(TO);
+  const int lane = threadIdx.x & 31;
+  u32 w[kWords];
+  result_words<TO>(v, w);
+#pragma unroll
+  for (int j = 0; j < kWords; j += 4) {
+    const u32 at = to + lane * kRowBytes + (((kFirst * sizeof(TO) / 16 + j / 4) ^ (lane & 7)) << 4);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[j]), "r"(w[j + 1]), "r"(w[j + 2]), "r"(w[j + 3]) : "memory");
+  }
+}
+
 // A warp's rows (a lane each) by up to 32 consecutive results, rows that start anywhere: sixteen words of sixteen rows change places among sixteen
 // lanes, then half a warp stores 64 consecutive bytes of a row (a lane's own row would be a sector per value: 100 us instead of 44 for 2631
 // rows of 1829 values).  All lanes call.
@@ -407,7 +432,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
   grid_wait();
   list_parts<kN>(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 63) / 64;
-  const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
+  const u32 n_tiles = static_cast<u32>(part[a.E]) * n_mt;
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
   zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
 
@@ -417,8 +442,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
     if (lane == 0 && rank == 0) {
       u32 it = 0, n_done = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1, ++n_done) {
-        const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+      for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1, ++n_done) {
+        const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
         const u32 idesc = t5_idesc(a.type, kAmn, false, kTileM, round32(t.n)), buf = n_done % kBuffers, d = tmem + buf * kN;
         ok = t5_wait(&b->sums_empty[buf], ((n_done / kBuffers) & 1) ^ 1);
         if (!ok) break;
@@ -447,9 +472,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
     const int quad = warp & 3;
     u32 n_done = 0;
     bool ok = true;
-    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1, ++n_done) {
-      const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m = static_cast<int>(id % n_mt) * kTileM + rank * 128 + quad * 32 + lane;
+    for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1, ++n_done) {
+      const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
+      const int m = static_cast<int>(id % static_cast<u32>(n_mt)) * kTileM + rank * 128 + quad * 32 + lane;
       const u32 buf = n_done % kBuffers;
       ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done / kBuffers) & 1));
       if (!ok) break;
@@ -522,7 +547,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
   grid_wait();
   list_parts<kTileN>(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 127) / 128;
-  const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
+  const u32 n_tiles = static_cast<u32>(part[a.E]) * n_mt;
   const u32 stage0 = smem_u32(stages), scale0 = smem_u32(scales), tmem = b->tmem;
   zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
 
@@ -534,7 +559,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
       u32 it = 0;
       bool ok = true;
       const u32 idesc = t5_idesc(a.type, false, false, 256, 256);
-      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+      for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
           const u32 s = it % kStages, sw = stage0 + s * kStage, sx = sw + kHalf, buf = it & 1, d = tmem + buf * 256;
           ok = t5_wait(&b->sums_empty[buf], ((it >> 1) & 1) ^ 1) && t5_wait(&b->full[s], (it / kStages) & 1);
@@ -555,9 +580,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
     } else if (warp == 3) {
       u32 it = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-        const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-        const int m0 = static_cast<int>(id % n_mt) * kTileM;
+      for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+        const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
+        const int m0 = static_cast<int>(id % static_cast<u32>(n_mt)) * kTileM;
         const float* ws = a.ws + static_cast<i64>(t.e) * a.ws_block;
         int row[4];
 #pragma unroll
@@ -582,9 +607,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
     const int quad = warp & 3, half = (warp - 4) >> 2, place = rank * 128 + quad * 32 + lane;
     u32 it = 0;
     bool ok = true;
-    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-      const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m = static_cast<int>(id % n_mt) * kTileM + half * 128;  // this warp's first row of W
+    for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+      const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
+      const int m = static_cast<int>(id % static_cast<u32>(n_mt)) * kTileM + half * 128;  // this warp's first row of W
       const bool some = place - lane < t.n;                              // whether this warp has places at all
       u64 acc[64];                                                       // two rows of W each
 #pragma unroll
@@ -675,7 +700,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
   grid_wait();
   list_parts<kFewN>(a.offsets, a.E, off, part, b->scan_tmp);
   const int n_mt = (a.n_m + kTileM - 1) / kTileM, n_kb = (a.n_k + 127) / 128;
-  const i64 n_tiles = static_cast<i64>(part[a.E]) * n_mt;
+  const u32 n_tiles = static_cast<u32>(part[a.E]) * n_mt;
   const u32 stage0 = smem_u32(stages), scale0 = smem_u32(scales), tmem = b->tmem;
   zero_rows(static_cast<TO*>(a.out), a.out_stride, off[a.E], a.places, a.n_m);
 
@@ -685,8 +710,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
     if (lane == 0 && rank == 0) {
       u32 it = 0;
       bool ok = true;
-      for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-        const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
+      for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+        const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
         const u32 idesc = t5_idesc(a.type, false, false, kTileM, round32(t.n));
         for (int kb = 0; kb < n_kb; ++kb, ++it) {
           const u32 s = it % kStages, sw = stage0 + s * kStage, sx = sw + kHalf, buf = it % kBuffers, d = tmem + buf * kFewN;
@@ -711,9 +736,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
   } else if (warp == 3) {
     u32 it = 0;
     bool ok = true;
-    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-      const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m0 = static_cast<int>(id % n_mt) * kTileM + rank * 128;
+    for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+      const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
+      const int m0 = static_cast<int>(id % static_cast<u32>(n_mt)) * kTileM + rank * 128;
       const float* ws = a.ws + static_cast<i64>(t.e) * a.ws_block;
       int row[kFewN / 32];
 #pragma unroll
@@ -735,9 +760,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
     const int quad = warp & 3, half = (warp - 4) >> 2;
     u32 it = 0;
     bool ok = true;
-    for (i64 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
-      const Part t = part_at(off, part, a.E, static_cast<int>(id / n_mt));
-      const int m = static_cast<int>(id % n_mt) * kTileM + rank * 128 + quad * 32 + lane;
+    for (u32 id = blockIdx.x >> 1; ok && id < n_tiles; id += gridDim.x >> 1) {
+      const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
+      const int m = static_cast<int>(id % static_cast<u32>(n_mt)) * kTileM + rank * 128 + quad * 32 + lane;
       const int each = round32(t.n) / 2, mine = min(each, t.n - half * each);  // places of this warp's half of the columns
       float acc[2][16] = {};
 #pragma unroll 1
@@ -785,51 +810,52 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
 // with a row per place); rows by index, and a column's last places, 16 bytes at a time by eight warps: what lies behind the last place is
 // not read but zero, so that a sum ends inside a stage whatever its neighbour holds.
 // Warps: 0 copies by tensor map, 1 matrix instructions, 2-5 results, 6-13 copies, 14 hands those over.
-// A tile of dW, and a walk over those of a pair of blocks that have places.
-struct DwTile {
-  i64 id;
-  int p0, p1, m0, j0, half;  // half: columns of X per block, 128 or 64
-};
+constexpr int kDwStages = 5;
+
+// A walk over a pair of blocks' tiles of dW, every role's own.  (No division by the tiles of a column on the way: with one, in 64 bits, walking took a role
+// 0.9 us a tile.)
 struct DwWalk {
   const DwArgs& a;
   const int* off;
-  int n_mt, n_per;
-  i64 n_tiles;
+  u32 n_mt, n_per, step_e, step_rest;  // tiles along m, tiles of a column, what the pairs' number is in these
+  u32 e, rest;
+  int p0, p1, m0, j0, half;            // places, first row and column, columns of X per block (128 or 64)
   __device__ __forceinline__ DwWalk(const DwArgs& args, const int* offsets) : a(args), off(offsets) {
+    const u32 pairs = gridDim.x >> 1, first = blockIdx.x >> 1;
     n_mt = (a.n_m + kTileM - 1) / kTileM;
     n_per = n_mt * ((a.n_j + kTileN - 1) / kTileN);
-    n_tiles = static_cast<i64>(a.E) * n_per;
+    step_e = pairs / n_per;
+    step_rest = pairs - step_e * n_per;
+    e = first / n_per;
+    rest = first - e * n_per;
+    look();
   }
-  __device__ __forceinline__ DwTile at(i64 id) const {
-    const int e = static_cast<int>(id / n_per), rest = static_cast<int>(id - static_cast<i64>(e) * n_per), j = rest / n_mt;
-    DwTile t;
-    t.id = id;
-    t.p0 = off[e];
-    t.p1 = off[e + 1];
-    t.m0 = (rest - j * n_mt) * kTileM;
-    t.j0 = j * kTileN;
-    t.half = a.n_j - t.j0 > 128 ? 128 : 64;
-    return t;
+  __device__ __forceinline__ bool more() const { return e < static_cast<u32>(a.E); }
+  __device__ __forceinline__ void look() {
+    if (!more()) return;
+    const u32 j = rest / n_mt;
+    p0 = off[e];
+    p1 = off[e + 1];
+    m0 = static_cast<int>(rest - j * n_mt) * kTileM;
+    j0 = static_cast<int>(j) * kTileN;
+    half = a.n_j - j0 > 128 ? 128 : 64;
   }
-  __device__ __forceinline__ DwTile first() const { return settle(blockIdx.x >> 1); }
-  __device__ __forceinline__ DwTile next(const DwTile& t) const { return settle(t.id + (gridDim.x >> 1)); }
-  __device__ __forceinline__ DwTile settle(i64 id) const {  // the next tile with places; id >= n_tiles: none
-    for (; id < n_tiles; id += gridDim.x >> 1) {
-      const DwTile t = at(id);
-      if (t.p0 < t.p1) return t;
-    }
-    DwTile none = {};
-    none.id = id;
-    return none;
+  __device__ __forceinline__ void next() {
+    e += step_e;
+    rest += step_rest;
+    if (rest >= n_per) { rest -= n_per; ++e; }
+    look();
   }
 };
 
 template <bool kGather, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
-    k_route_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const DwArgs a) {
+    k_route_dw(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_out, const DwArgs a) {
+  constexpr int kStages = kDwStages;
   extern __shared__ char t5_sm[];
   char* stages = t5_align(t5_sm);
-  T5Block* b = reinterpret_cast<T5Block*>(stages + kStages * kStage);
+  char* results = stages + kStages * kStage;  // two for each result warp
+  T5Block* b = reinterpret_cast<T5Block*>(results + 8 * kOutBytes);
   int* off = reinterpret_cast<int*>(b + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const u32 rank = cluster_rank();
@@ -837,7 +863,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
   grid_wait();
   for (int e = threadIdx.x; e <= a.E; e += blockDim.x) off[e] = static_cast<int>(a.offsets[e]);
   __syncthreads();
-  const DwWalk walk(a, off);
   const u32 stage0 = smem_u32(stages), tmem = b->tmem;
   constexpr u32 kBlock = 64 * kRowBytes;  // 64 places of 64 values
 
@@ -845,7 +870,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
     if (lane == 0) {
       u32 it = 0;
       bool ok = true;
-      for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t)) {
+      for (DwWalk t(a, off); ok && t.more(); t.next()) {
         const int m = t.m0 + rank * 128, j = t.j0 + rank * t.half;
         for (int p = t.p0; p < t.p1; p += 64, ++it) {
           const u32 s = it % kStages, sa = stage0 + s * kStage, sb = sa + kHalf;
@@ -866,7 +891,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
       }
       if (!ok) {
         dev_set_error(a.err, kDevTimeout);
-        if (rank == 0) t5_drain_copies(b, it);
+        if (rank == 0) t5_drain_copies<kStages>(b, it);
       }
     }
     __syncwarp();
@@ -874,7 +899,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
     if (lane == 0 && rank == 0) {
       u32 it = 0, n_done = 0;
       bool ok = true;
-      for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t), ++n_done) {
+      for (DwWalk t(a, off); ok && t.more(); t.next()) {
+        if (t.p0 >= t.p1) continue;
         const u32 idesc = t5_idesc(a.type, true, true, kTileM, 2 * t.half), buf = n_done & 1, d = tmem + buf * kTileN;
         ok = t5_wait(&b->sums_empty[buf], ((n_done >> 1) & 1) ^ 1);
         if (!ok) break;
@@ -890,6 +916,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
           t5_commit(&b->empty[s]);
         }
         if (ok) t5_commit(&b->sums_full[buf]);
+        ++n_done;
       }
       if (!ok) {
         dev_set_error(a.err, kDevTimeout);
@@ -901,8 +928,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
     if (lane == 0) {
       u32 it = 0;
       bool ok = true;
-      for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t))
-        for (int p = t.p0; ok && p < t.p1; p += 64, ++it) ok = hand_over<>(b, it);
+      for (DwWalk t(a, off); ok && t.more(); t.next())
+        for (int p = t.p0; ok && p < t.p1; p += 64, ++it) ok = hand_over<kStages>(b, it);
       if (!ok) dev_set_error(a.err, kDevTimeout);
     }
     __syncwarp();
@@ -910,9 +937,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
     // sixteen lanes have a row: 256 bytes of dP, 256 (or 128) of X; a thread the rows r0 + 16 i of a stage
     const int thread = threadIdx.x - 192, c = thread & 15, r0 = thread >> 4;
     const u32 at = (c >> 3) * kBlock + r0 * kRowBytes + (((c & 7) ^ (r0 & 7)) << 4);  // (rows r0 + 16 i: the same swizzle)
-    CopyQueue<> queue(b);
+    CopyQueue<kStages> queue(b);
     bool ok = true;
-    for (DwTile t = walk.first(); ok && t.id < walk.n_tiles; t = walk.next(t)) {
+    for (DwWalk t(a, off); ok && t.more(); t.next()) {
       const int m = t.m0 + rank * 128 + c * 8, j = t.j0 + rank * t.half + c * 8;
       const u32 m_bytes = 2 * max(0, min(8, a.n_m - m)), j_bytes = 2 * max(0, min(8, a.n_j - j));
       const char* dp = a.dp + (m_bytes ? 2 * static_cast<i64>(m) : 0);
@@ -954,24 +981,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   } else if (warp >= 2) {
     const int quad = warp & 3;
-    u32 n_done = 0;
+    u32 n_done = 0, run = 0;
     bool ok = true;
-    for (i64 id = blockIdx.x >> 1; ok && id < walk.n_tiles; id += gridDim.x >> 1) {
-      const DwTile t = walk.at(id);
-      const int e = static_cast<int>(id / walk.n_per), m = t.m0 + rank * 128 + quad * 32 + lane, n = min(kTileN, a.n_j - t.j0);
+    for (DwWalk t(a, off); ok && t.more(); t.next()) {
+      const int e = static_cast<int>(t.e), m = t.m0 + rank * 128 + quad * 32 + lane, n = min(kTileN, a.n_j - t.j0);
       TO* out = static_cast<TO*>(a.out) + static_cast<i64>(e) * a.out_block + static_cast<i64>(m - lane) * a.out_stride + t.j0;
       const u32 buf = n_done & 1;
       if (t.p0 < t.p1) {
         ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done >> 1) & 1));
         if (!ok) break;
         t5_fence_after();
-        for (int c = 0; c < n; c += 32) {
-          u32 v[32];
-          t5_ld32(v, tmem + buf * kTileN + c + (static_cast<u32>(quad * 32) << 16));
-          t5_wait_ld();
-          if (a.out_align >= 16 && n - c >= 32) {
-            if (m < a.n_m) store_run(out + lane * a.out_stride + c, a.out_align, v);
-          } else {
+        const u32 sums = tmem + buf * kTileN + (static_cast<u32>(quad * 32) << 16);
+        if (a.out_align >= 16) {
+          for (int c = 0; c < n; c += kOutRun<TO>) {
+            const u32 slot = smem_u32(results) + (quad * 2 + (run & 1)) * kOutBytes;
+            if (lane == 0) tma_store_read<1>();
+            __syncwarp();
+            u32 v[32];
+            t5_ld32(v, sums + c);
+            t5_wait_ld();
+            lay_down<TO, 0>(slot, v);
+            if constexpr (sizeof(TO) == 2) {
+              t5_ld32(v, sums + c + 32);
+              t5_wait_ld();
+              lay_down<TO, 32>(slot, v);
+            }
+            fence_to_matrix();
+            __syncwarp();
+            if (lane == 0) tma_store_3d(&map_out, t.j0 + c, m - lane, e, slot);
+            ++run;
+          }
+        } else {
+          for (int c = 0; c < n; c += 32) {
+            u32 v[32];
+            t5_ld32(v, sums + c);
+            t5_wait_ld();
             store_turned(out + c, a.out_stride, a.n_m - (m - lane), n - c, a.out_align, v);
           }
         }
@@ -990,6 +1034,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
           }
       }
     }
+    if (lane == 0) tma_store_done();
     if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
   }
   __syncwarp();

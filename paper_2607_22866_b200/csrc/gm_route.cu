@@ -113,7 +113,7 @@ static int make_map(CUtensorMap* map, int dtype, int rank, const void* base, con
   PFN_cuTensorMapEncodeTiled_v12000 encode;
   GM_TRY(encoder(&encode));
   const uint32_t ones[3] = {1, 1, 1};
-  const CUtensorMapDataType type = dtype == GM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : dtype == GM_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  const CUtensorMapDataType type = dtype == GM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : dtype == GM_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : dtype == GM_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
   const CUresult rc = encode(map, type, rank, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (rc != CUDA_SUCCESS) return fail(GM_ERR_CUDA, "cuTensorMapEncodeTiled: error " + std::to_string(static_cast<int>(rc)));
@@ -198,6 +198,16 @@ static int map_rows(CUtensorMap* map, gm_dense* rows, uint32_t at_a_time, Scratc
   const uint64_t strides[1] = {static_cast<uint64_t>(M.n_rows > 1 ? M.row_stride * es : (M.n_cols * es + 15) / 16 * 16)};
   const uint32_t box[2] = {static_cast<uint32_t>(kRowBytes / es), at_a_time};
   return make_map(map, M.dtype, 2, M.data, dims, strides, box);
+}
+
+// A map of a result's blocks (or of one matrix), written 32 rows by 128 bytes at a time.  Only where the rows' addresses allow it (out_align).
+static int map_out(CUtensorMap* map, const gm_dense& M) {
+  const i64 es = static_cast<i64>(elem_size(M.dtype));
+  const uint64_t row = static_cast<uint64_t>(M.n_rows > 1 ? M.row_stride * es : (M.n_cols * es + 15) / 16 * 16);
+  const uint64_t dims[3] = {static_cast<uint64_t>(M.n_cols), static_cast<uint64_t>(M.n_rows), static_cast<uint64_t>(M.n_blocks)};
+  const uint64_t strides[2] = {row, M.n_blocks > 1 ? static_cast<uint64_t>(M.block_stride * es) : row * M.n_rows};
+  const uint32_t box[3] = {static_cast<uint32_t>(kRowBytes / es), 32, 1};
+  return make_map(map, M.dtype, 3, M.data, dims, strides, box);
 }
 
 static int route_ready(const gm_route* r) {
@@ -571,7 +581,10 @@ int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dens
     a.type = dP->dtype == GM_BF16 ? 1 : 0;
     a.err = route->err;
     const i64 tiles = static_cast<i64>(a.E) * ((a.n_m + kTileM - 1) / kTileM) * ((a.n_j + kTileN - 1) / kTileN);
-    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 480, kT5Smem<kTileN> + (a.E + 1) * 4, st, map_p, map_x, a); };
+    CUtensorMap out_map = map_p;  // (used where the rows of dW are aligned)
+    if (a.out_align >= 16) GM_TRY(map_out(&out_map, *dW));
+    const size_t smem = static_cast<size_t>(kDwStages) * kStage + 8 * kOutBytes + 1024 + sizeof(T5Block) + (a.E + 1) * 4;
+    const auto go = [&]<auto kernel>() { return launch_t5<kernel>(tiles, num_sms, 480, smem, st, map_p, map_x, out_map, a); };
     switch (dW->dtype) {
       case GM_F32: return by_entry ? go.template operator()<k_route_dw<false, float>>() : go.template operator()<k_route_dw<true, float>>();
       case GM_BF16: return by_entry ? go.template operator()<k_route_dw<false, __nv_bfloat16>>() : go.template operator()<k_route_dw<true, __nv_bfloat16>>();

@@ -55,6 +55,20 @@ __device__ __forceinline__ void tma_load_3d(u32 dst, const CUtensorMap* map, int
                : "memory");
 }
 
+// From this block's memory into a result, by tensor map: what lies outside is not written.  One thread; the memory may be written again after
+// tma_store_read(), and the block leave after tma_store_done().
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, u32 src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n\tcp.async.bulk.commit_group;" ::"l"(map), "r"(x), "r"(y), "r"(src)
+               : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, u32 src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];\n\tcp.async.bulk.commit_group;" ::"l"(map), "r"(x), "r"(y), "r"(z),
+               "r"(src)
+               : "memory");
+}
+template <int kLeft> __device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ void tma_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // 16 bytes by the thread itself, of which the first `bytes` (0 .. 16) are read and the others become zero
 __device__ __forceinline__ void copy16(u32 dst, const void* src, u32 bytes) {
   asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
