@@ -115,10 +115,11 @@ struct SumArgs {
 
 constexpr int kSumThreads = 128;
 
-// kUnits: runs of columns per thread, kSumThreads runs apart; eight loads are in flight, for 8 / kUnits entries.
+// kUnits: runs of columns per thread, kSumThreads runs apart; eight loads of 16 bytes (or sixteen of one value) are in flight, for as many
+// entries as that leaves.
 template <typename TI, typename TO, bool kVec, int kUnits>
 __global__ void __launch_bounds__(kSumThreads) k_route_sum(const SumArgs a, int n_chunks) {
-  constexpr int kCols = kVec ? 16 / sizeof(TI) : 1, kEntries = 8 / kUnits, kStep = kSumThreads * kCols;
+  constexpr int kCols = kVec ? 16 / sizeof(TI) : 1, kEntries = (kVec ? 8 : 16) / kUnits, kStep = kSumThreads * kCols;
   const i64 i = blockIdx.x / n_chunks;
   const int c = static_cast<int>(blockIdx.x % n_chunks) * kUnits * kStep + threadIdx.x * kCols;
   grid_launch_next();

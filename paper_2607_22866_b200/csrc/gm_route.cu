@@ -392,7 +392,7 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
   const bool vec = rows_aligned(P) && rows_aligned(Y);
   // eight loads in flight per thread: of as many entries as rows have on average, and the rest of other columns
   const i64 mean = (r->nnz + r->n_rows - 1) / r->n_rows;
-  const int columns = mean > 4 ? 1 : mean > 2 ? 2 : mean > 1 ? 4 : 8;
+  const int columns = vec ? (mean > 4 ? 1 : mean > 2 ? 2 : mean > 1 ? 4 : 8) : (mean > 2 ? 4 : 8);
   const i64 per = kSumThreads * columns * (vec ? 16 / static_cast<i64>(elem_size(P.dtype)) : 1), chunks = (a.width + per - 1) / per;
   GM_TRY(sum_grid(chunks * r->n_rows, "sum"));
   const auto go = [&](auto kernel) {
@@ -402,7 +402,11 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
     using TI = std::remove_pointer_t<decltype(ti)>;
     using TO = std::remove_pointer_t<decltype(to)>;
     const auto aligned = [&]<bool kVec>() {
-      return columns == 1 ? go(k_route_sum<TI, TO, kVec, 1>) : columns == 2 ? go(k_route_sum<TI, TO, kVec, 2>) : columns == 4 ? go(k_route_sum<TI, TO, kVec, 4>) : go(k_route_sum<TI, TO, kVec, 8>);
+      if constexpr (kVec) {
+        if (columns == 1) return go(k_route_sum<TI, TO, true, 1>);
+        if (columns == 2) return go(k_route_sum<TI, TO, true, 2>);
+      }
+      return columns == 4 ? go(k_route_sum<TI, TO, kVec, 4>) : go(k_route_sum<TI, TO, kVec, 8>);
     };
     return vec ? aligned.template operator()<true>() : aligned.template operator()<false>();
   };
