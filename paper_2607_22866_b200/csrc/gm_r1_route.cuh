@@ -3,9 +3,10 @@
 //   offsets[e]  first place of column e (e = E: entries whose column is outside [0, E), behind all others)
 //   rows[p], order[p]   row and index of the entry at place p;   pos[q] the place of entry q
 //
-// A counting sort in one launch: a cluster of up to 16 blocks shares the entries, every warp a run of consecutive ones with counters of its
+// A counting sort, in one launch where there are few entries: a cluster of up to 16 blocks shares them, every warp a run of consecutive ones with counters of its
 // own in shared memory (so that places do not depend on the order in which anything runs), the blocks' sums go through
-// distributed shared memory.  Bound by latency: two walks over the entries and three cluster barriers.
+// distributed shared memory.  Bound by latency, and by its own instructions, which every launch fetches anew: the walks are loops that are
+// not unrolled (19 us with them unrolled by eight, for 131072 entries).
 #pragma once
 #include <cooperative_groups.h>
 
@@ -16,31 +17,32 @@ namespace gm {
 constexpr int kRouteMaxCols = 2048;
 constexpr int kRouteThreads = 1024;
 constexpr int kRouteBlocks = 16;     // where a cluster of so many fits the device, else 8
-constexpr int kRouteAhead = 8;  // loads of columns under way
+// With more than kRouteWide entries in at most kRouteWideCols columns: as many blocks, which need a launch for their sums (131072 entries in 64
+// columns: 15.7 us, 21.6 by the cluster; 32768 entries: 10.1 against 8.8; 240000 in 2000 columns: 154 against
+// 52, for every block reads all blocks' sums).
+constexpr int kRouteWideBlocks = 128;
+constexpr int kRouteWideThreads = 256;
+constexpr i64 kRouteWide = 65536;
+constexpr int kRouteWideCols = 128;
 constexpr int kRouteCounterBytes = 200 * 1024;
 
-// Rows of a warp's 32 consecutive entries qb + lane (those below q1), given a row r that does not lie behind the first one's; returns the last
-// one's.  The next rows' starts are looked at 32 at a time; where rows without entries follow in large numbers, by bisection.
-__device__ __forceinline__ int route_rows(const i64* __restrict__ row_ptr, int n_rows, i64 q1, i64 qb, int r, int* row) {
-  const int lane = threadIdx.x & 31;
-  const i64 q = qb + lane;
-  bool open = q < q1;
-  *row = r;
-  for (int round = 0; round < 2 && __any_sync(0xffffffffu, open); ++round) {
-    const int base = r + 32 * round;  // rows base .. base + 31: their ends
-    const i64 end = base + 1 + lane <= n_rows ? row_ptr[base + 1 + lane] : LLONG_MAX;
-    int k = 0;  // ends that are not behind q
+// The end of row r + lane, as an int (there are fewer than 2^31 entries); what lies behind the last row ends nowhere.
+__device__ __forceinline__ int route_end(const i64* __restrict__ row_ptr, int n_rows, int r) {
+  const int i = r + static_cast<int>(threadIdx.x & 31);
+  return i < n_rows ? static_cast<int>(min(row_ptr[i + 1], static_cast<i64>(INT_MAX))) : INT_MAX;
+}
+// The row of an entry that the window of ends does not reach (many rows without entries).
+__device__ __noinline__ int route_far(const i64* __restrict__ row_ptr, int n_rows, int q) {
+  return static_cast<int>(last_le(row_ptr, 0, n_rows - 1, q));
+}
+// Rows of a warp's 32 consecutive entries, q this lane's, from a row r that does not lie behind the first one's and the ends of the 32 rows from
+// there on.
+__device__ __forceinline__ int route_rows(const i64* __restrict__ row_ptr, int n_rows, int q, int r, int end) {
+  int k = 0;  // ends that are not behind q
 #pragma unroll
-    for (int step = 16; step > 0; step >>= 1)
-      if (__shfl_sync(0xffffffffu, end, k + step - 1) <= q) k += step;
-    const i64 at = __shfl_sync(0xffffffffu, end, k);
-    if (open && (k < 31 || at > q)) {
-      *row = min(n_rows - 1, base + k);
-      open = false;
-    }
-  }
-  if (open) *row = static_cast<int>(last_le(row_ptr, min(n_rows - 1, r + 64), n_rows - 1, q));
-  return __shfl_sync(0xffffffffu, *row, static_cast<int>(min(static_cast<i64>(31), q1 - qb - 1)));
+  for (int step = 16; step > 0; step >>= 1)
+    if (__shfl_sync(0xffffffffu, end, k + step - 1) <= q) k += step;
+  return __shfl_sync(0xffffffffu, end, k) > q ? min(n_rows - 1, r + k) : route_far(row_ptr, n_rows, q);
 }
 
 // The last row that starts at or before entry q: looked for where it would be if all rows were equally long, then by bisection.
@@ -50,8 +52,7 @@ __device__ __forceinline__ int route_first_row(const i64* __restrict__ row_ptr, 
   const i64 start = g + lane <= n_rows ? row_ptr[g + lane] : LLONG_MAX;
   const u32 before = __ballot_sync(0xffffffffu, start <= q);  // (starts ascend: a run of low bits)
   const int k = __popc(before);
-  if (k > 0 && (k < 32 || g + 32 >= n_rows)) return min(n_rows - 1, g + k - 1);
-  return static_cast<int>(last_le(row_ptr, 0, n_rows - 1, q));
+  return k > 0 && (k < 32 || g + 32 >= n_rows) ? min(n_rows - 1, g + k - 1) : route_far(row_ptr, n_rows, static_cast<int>(q));
 }
 
 __host__ __device__ inline int route_warps(int cols) {
@@ -60,8 +61,29 @@ __host__ __device__ inline int route_warps(int cols) {
 }
 inline size_t route_smem(int cols, int warps) { return static_cast<size_t>(warps + 2) * (cols + 1) * 4; }
 
+// Each block's entries per column, for k_route_plan<false> with as many blocks and warps: sums[column * blocks + block].
+__global__ void __launch_bounds__(kRouteThreads, 1) k_route_count(const int32_t* __restrict__ col, i64 nnz, int E, u32* __restrict__ sums) {
+  extern __shared__ u32 route_sm[];
+  const int bins = E + 1, warps = blockDim.x >> 5;
+  grid_launch_next();
+  for (int e = threadIdx.x; e < bins; e += blockDim.x) route_sm[e] = 0;
+  __syncthreads();
+  grid_wait();
+  const i64 n_warps = static_cast<i64>(gridDim.x) * warps, per = (nnz + n_warps - 1) / n_warps;  // (the same shares as there)
+  const int q0 = static_cast<int>(min(nnz, static_cast<i64>(blockIdx.x) * warps * per)), q1 = static_cast<int>(min(nnz, q0 + warps * per));
+#pragma unroll 4
+  for (int q = q0 + static_cast<int>(threadIdx.x); q < q1; q += blockDim.x) {
+    const int c = col[q];
+    atomicAdd(&route_sm[static_cast<u32>(c) < static_cast<u32>(E) ? c : E], 1u);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < bins; e += blockDim.x) sums[static_cast<i64>(e) * gridDim.x + blockIdx.x] = route_sm[e];
+}
+
+// kCluster: the blocks are one cluster and tell each other their sums; else these come from k_route_count.
+template <bool kCluster>
 __global__ void __launch_bounds__(kRouteThreads, 1) k_route_plan(const i64* __restrict__ row_ptr, const int32_t* __restrict__ col,
-                                                              int n_rows, i64 nnz, int E, i64* __restrict__ offsets,
+                                                              int n_rows, i64 nnz, int E, const u32* __restrict__ sums, i64* __restrict__ offsets,
                                                               int32_t* __restrict__ rows, int32_t* __restrict__ order,
                                                               int32_t* __restrict__ pos) {
   namespace cg = cooperative_groups;
@@ -76,27 +98,17 @@ __global__ void __launch_bounds__(kRouteThreads, 1) k_route_plan(const i64* __re
   for (int e = lane; e < bins; e += 32) cnt[e] = 0;
   grid_wait();
   const i64 n_warps = static_cast<i64>(gridDim.x) * warps, per = (nnz + n_warps - 1) / n_warps;
-  const i64 q0 = min(nnz, (static_cast<i64>(blockIdx.x) * warps + warp) * per), q1 = min(nnz, q0 + per);
-  // the first columns and their rows stay in registers for the second walk
-  int c0[kRouteAhead], row0[kRouteAhead];
-#pragma unroll
-  for (int j = 0; j < kRouteAhead; ++j) c0[j] = q0 + 32 * j + lane < q1 ? col[q0 + 32 * j + lane] : 0;
-  int r = q0 < q1 ? route_first_row(row_ptr, n_rows, nnz, q0) : 0;
+  const int q0 = static_cast<int>(min(nnz, (static_cast<i64>(blockIdx.x) * warps + warp) * per)), q1 = static_cast<int>(min(nnz, q0 + per));
   __syncwarp();
-#pragma unroll
-  for (int j = 0; j < kRouteAhead; ++j)
-    if (q0 + 32 * j + lane < q1) atomicAdd(&cnt[static_cast<u32>(c0[j]) < static_cast<u32>(E) ? c0[j] : E], 1u);
-#pragma unroll
-  for (int j = 0; j < kRouteAhead; ++j)
-    if (q0 + 32 * j < q1) r = route_rows(row_ptr, n_rows, q1, q0 + 32 * j, r, &row0[j]);
-  for (i64 qb = q0 + 32 * kRouteAhead; qb < q1; qb += 32 * kRouteAhead) {
-    int c[kRouteAhead];
-#pragma unroll
-    for (int j = 0; j < kRouteAhead; ++j) c[j] = qb + 32 * j + lane < q1 ? col[qb + 32 * j + lane] : 0;
-#pragma unroll
-    for (int j = 0; j < kRouteAhead; ++j)
-      if (qb + 32 * j + lane < q1) atomicAdd(&cnt[static_cast<u32>(c[j]) < static_cast<u32>(E) ? c[j] : E], 1u);
+#pragma unroll 4
+  for (int q = q0 + lane; q < q1; q += 32) {
+    const int c = col[q];
+    atomicAdd(&cnt[static_cast<u32>(c) < static_cast<u32>(E) ? c : E], 1u);
   }
+  // on their way while the blocks add up: this warp's first columns and rows
+  int c = q0 + lane < q1 ? col[q0 + lane] : 0;
+  int r = q0 < q1 ? route_first_row(row_ptr, n_rows, nnz, q0) : 0;
+  int end = route_end(row_ptr, n_rows, r);
   __syncthreads();
   for (int e = threadIdx.x; e < bins; e += blockDim.x) {
     u32 s = 0;
@@ -108,22 +120,45 @@ __global__ void __launch_bounds__(kRouteThreads, 1) k_route_plan(const i64* __re
     }
     sum[e] = s;
   }
-  cluster.sync();
+  if (kCluster) {
+    cluster.sync();
+  } else {  // a warp adds up a column's blocks
+    __syncthreads();
+    const int blocks = static_cast<int>(gridDim.x), mine = static_cast<int>(blockIdx.x);
+#pragma unroll 4
+    for (int e = warp; e < bins; e += warps) {
+      u32 before = 0, all = 0;
+      for (int i = lane; i < blocks; i += 32) {
+        const u32 v = sums[static_cast<i64>(e) * blocks + i];
+        all += v;
+        if (i < mine) before += v;
+      }
+      all = warp_sum(all);
+      before = warp_sum(before);
+      if (lane == 0) { sum[e] = all; base[e] = before; }
+    }
+    __syncthreads();
+  }
   u32 before = 0;
   for (int e0 = 0; e0 < bins; e0 += blockDim.x) {
     const int e = e0 + threadIdx.x;
     u32 all = 0, mine = 0;
     if (e < bins) {
-      for (unsigned b0 = 0; b0 < gridDim.x; b0 += 4) {  // (1, 2 or a multiple of four blocks)
-        u32 v[4];
+      if (kCluster) {
+        for (unsigned b0 = 0; b0 < gridDim.x; b0 += 4) {  // (1, 2 or a multiple of four blocks)
+          u32 v[4];
 #pragma unroll
-        for (unsigned i = 0; i < 4; ++i) v[i] = cluster.map_shared_rank(sum, min(b0 + i, gridDim.x - 1))[e];
+          for (unsigned i = 0; i < 4; ++i) v[i] = cluster.map_shared_rank(sum, min(b0 + i, gridDim.x - 1))[e];
 #pragma unroll
-        for (unsigned i = 0; i < 4; ++i)
-          if (b0 + i < gridDim.x) {
-            if (b0 + i < blockIdx.x) mine += v[i];
-            all += v[i];
-          }
+          for (unsigned i = 0; i < 4; ++i)
+            if (b0 + i < gridDim.x) {
+              if (b0 + i < blockIdx.x) mine += v[i];
+              all += v[i];
+            }
+        }
+      } else {
+        all = sum[e];
+        mine = base[e];
       }
     }
     u32 total;
@@ -135,33 +170,26 @@ __global__ void __launch_bounds__(kRouteThreads, 1) k_route_plan(const i64* __re
     }
     __syncthreads();
   }
-  cluster.sync();  // (no block leaves while another still reads its sums)
-  for (i64 qa = q0; qa < q1; qa += 32 * kRouteAhead) {
-    if (qa > q0) {
-#pragma unroll
-      for (int j = 0; j < kRouteAhead; ++j) c0[j] = qa + 32 * j + lane < q1 ? col[qa + 32 * j + lane] : 0;
-#pragma unroll
-      for (int j = 0; j < kRouteAhead; ++j)
-        if (qa + 32 * j < q1) r = route_rows(row_ptr, n_rows, q1, qa + 32 * j, r, &row0[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < kRouteAhead; ++j) {
-      const i64 q = qa + 32 * j + lane;
-      if (qa + 32 * j < q1) {
-        const bool in = q < q1;
-        const int e = in ? (static_cast<u32>(c0[j]) < static_cast<u32>(E) ? c0[j] : E) : -1;
-        const u32 peers = __match_any_sync(0xffffffffu, e);
-        u32 place = 0;
-        if (in) place = base[e] + cnt[e] + __popc(peers & lanemask_lt());
-        __syncwarp();
-        if (in && (peers & lanemask_lt()) == 0) cnt[e] += __popc(peers);
-        __syncwarp();
-        if (in) {
-          pos[q] = static_cast<int32_t>(place);
-          order[place] = static_cast<int32_t>(q);
-          rows[place] = row0[j];
-        }
-      }
+  if (kCluster) cluster.sync();  // (no block leaves while another still reads its sums)
+#pragma unroll 1
+  for (int qb = q0; qb < q1; qb += 32) {
+    const int q = qb + lane;
+    const bool in = q < q1;
+    const int e = in ? (static_cast<u32>(c) < static_cast<u32>(E) ? c : E) : -1;
+    c = q + 32 < q1 ? col[q + 32] : 0;
+    const int row = route_rows(row_ptr, n_rows, min(q, q1 - 1), r, end);
+    r = __shfl_sync(0xffffffffu, row, 31);
+    end = route_end(row_ptr, n_rows, r);
+    const u32 peers = __match_any_sync(0xffffffffu, e), below = peers & lanemask_lt();
+    u32 place = 0;
+    if (in) place = base[e] + cnt[e] + __popc(below);
+    __syncwarp();
+    if (in && below == 0) cnt[e] += __popc(peers);
+    __syncwarp();
+    if (in) {
+      pos[q] = static_cast<int32_t>(place);
+      order[place] = q;
+      rows[place] = row;
     }
   }
 }

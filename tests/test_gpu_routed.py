@@ -87,7 +87,7 @@ def product_reference(R, X, W, by_entry):
 ROUTES = [  # n, E, k, drop, empty, skew
     (1, 1, 1, 0.0, 0.0, 0.0), (1, 7, 5, 0.0, 0.0, 0.0), (3, 40, 4, 0.2, 0.3, 0.0), (0, 3, 2, 0.0, 0.0, 0.0), (5, 3, 2, 1.0, 0.0, 0.0),
     (64, 8, 3, 0.1, 0.5, 1.0), (700, 5, 3, 0.05, 0.1, 2.0), (1025, 1, 1, 0.0, 0.0, 0.0), (2000, 33, 6, 0.0, 0.0, 0.7), (40, 2048, 8, 0.1, 0.0, 0.0),
-    (30000, 130, 9, 0.1, 0.1, 1.0), (5000, 2048, 9, 0.01, 0.0, 0.5), (100, 600, 300, 0.0, 0.9, 0.0),
+    (30000, 130, 9, 0.1, 0.1, 1.0), (20000, 100, 9, 0.1, 0.1, 1.0), (70000, 1, 1, 0.3, 0.0, 0.0), (300000, 128, 1, 0.0, 0.6, 0.0), (5000, 2048, 9, 0.01, 0.0, 0.5), (100, 600, 300, 0.0, 0.9, 0.0),
 ]
 
 
