@@ -5,8 +5,8 @@
 //
 // A counting sort, in one launch where there are few entries: a cluster of up to 16 blocks shares them, every warp a run of consecutive ones with counters of its
 // own in shared memory (so that places do not depend on the order in which anything runs), the blocks' sums go through
-// distributed shared memory.  Bound by latency, and by its own instructions, which every launch fetches anew: the walks are loops that are
-// not unrolled (19 us with them unrolled by eight, for 131072 entries).
+// distributed shared memory.  Bound by latency, and with few entries by its own instructions, which every launch fetches anew: the walks are loops
+// that are not unrolled (a few entries 3.9 us, 4.7 with them unrolled by eight).
 #pragma once
 #include <cooperative_groups.h>
 

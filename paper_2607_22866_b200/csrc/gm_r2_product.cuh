@@ -6,9 +6,13 @@
 //
 // All three work on tiles of 256 x 256 sums, a pair of blocks (of neighbouring SMs) each: either block brings in half of both
 // operands and keeps half of the sums, 256 columns by 128 lanes of its tensor memory.  A single block per 128 x 256 tile moves 1.5
-// times the bytes through shared memory per product, which then bounds it (1.03 against 1.3 PFLOP/s at 32768 x 2048 x 2048).
+// times the bytes through shared memory per product, which then bounds it (268 against 227 us at 32768 places x 2048 x 2048).
+// What bounds the pairs is the way from L2 to the SMs: 32 KB a stage and block, at 85 GB/s per SM 380 ns, which is the library's matrix
+// product's pace (1.62 PFLOP/s), too; these reach 1.46 PFLOP/s with 256 places a tile (16384 places x 2048 x 4096, a row per place), 1.31 with
+// rows by index, 1.15 with the 205 places that a tile holds on average at 32768 places in 64 columns of skewed popularity.
 // The places are the instruction's N: a column's places are cut into equal parts, and a part of 33 places costs matrix time for 64.
-// The sums have two buffers, so that the results of one tile are taken out while the next one is summed up.
+// The sums have two buffers, so that the results of one tile are taken out while the next one is summed up.  Every role of a block finds its
+// tiles by itself; that costs each of them a fraction of a microsecond a tile, and took up to 0.9 with divisions in 64 bits.
 //
 // Rows of X are fetched by index with 16-byte asynchronous copies of four warps.  (Tensor-map loads of four rows by index took
 // about 50 cycles each however many warps issued them, four times what the matrix instructions take for those rows.)
@@ -174,8 +178,10 @@ __device__ __forceinline__ void t5_drain_matrix(T5Block* b) {
 }
 
 // Rows by index: the copying threads go as far ahead as there are stages.  Their copies arrive on the stage's own barrier of the block;
-// one thread that has no copies under way itself makes them visible to the matrix instructions and tells the leader.  (A copying
-// thread's own fence waits for all its copies, the next stages' too: 43 us instead of 25 for a product of one row.)
+// one thread that has no copies under way itself makes them visible to the matrix instructions and tells the leader (614 us for
+// 32768 places x 2048 x 2048, 742 with a fence by every copying thread, which waits for all its copies; both before the arrivals at the
+// leader's barrier were left at the default scope: releasing at cluster scope takes 0.6 us a stage, 614 -> 250 us.  What has to be seen across
+// blocks is the barrier alone: each block's matrix unit reads that block's own memory).
 template <int kStages = gm::kStages>
 struct CopyQueue {
   T5Block* b;
@@ -358,7 +364,8 @@ __device__ __forceinline__ void store_run(TO* __restrict__ out, int align, const
   }
 }
 // A warp's 32 rows (a lane each) by kOutRun results: laid down in shared memory (32 rows of 128 bytes, swizzled as the tensor map wants it), from
-// where one copy writes whole lines.  A lane's own row of 32 bytes per store took 3.3 us a tile of 256 x 256, more than a short sum's products.
+// where one copy writes whole lines.  With 32 bytes of its own row per lane and store, a tile of 256 x 256 took 2.8 us instead of 2.05, more than a
+// short sum's products.
 constexpr int kOutBytes = 32 * kRowBytes;
 template <typename TO> constexpr int kOutRun = kRowBytes / sizeof(TO);
 template <typename TO, int kFirst>  // 32 sums that are the values kFirst .. kFirst + 31 of the rows
@@ -503,9 +510,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
 //
 // Here the places are the lanes (the instruction's M) and the rows of W the columns, so that a thread has one place: its scale times
 // that of the 128 rows of W is one number per thread and block of k, and the rows of the result are stored in whole runs.  (With the rows of W
-// as lanes a scale per column has to be read from shared memory for every sum: 547 us instead of 385 at 32768 x 4096 x 2048.)
-// What bounds it is the way of the sums out of tensor memory: about 1100 cycles per block of k and tile, of which the matrix
-// instructions need 512.
+// as lanes a scale per column has to be read from shared memory for every sum: 547 against 457 us at 32768 places x 4096 x 2048, 397 by now.)
+// What bounds it is the way of the sums out of tensor memory and through the FP32 units: 0.69 us per block of k and tile, of which the matrix
+// instructions need 0.28; without either's work 0.55 us remain, the way from one buffer's last product to its next one.
 // kRowScales: W has scales for each row and 128 values, which are read from shared memory, else for each 128 rows.
 // Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 3 scales, 4-11 results.  The results' registers
 // are what the others give up: 512 threads begin with 128 each.

@@ -242,9 +242,9 @@ static size_t product_smem(int E, bool bits8) {
 }
 static_assert(std::max(kT5Smem<kTileN> + kScaleSmem<kTileN>, kT5Smem<kFewN> + kScaleSmem<kFewN>) + (kRouteMaxCols + 1) * 8 <= kMostSmem, "fits a block's shared memory");
 
-// Whether tiles of few places are the better ones: as long as a column has at most half of such a tile's on average (the tiles of
-// 256 places then hold little, and give the weights fewer stages and buffers).
-static bool few_places(const gm_route* r) { return r->nnz <= static_cast<i64>(kFewN / 2) * std::min<i64>(r->E, r->nnz); }
+// Whether tiles of few places are the better ones: while a column has at most three quarters of such a tile's on average (64 columns of 1536 x 4096: with 8
+// places each 158 us against 165 with tiles of 256, in 8 bits 98 against 125; with 48 164 : 169 and 106 : 133, with 64 180 : 171 and 135 : 133).
+static bool few_places(const gm_route* r) { return r->nnz <= static_cast<i64>(kFewN * 3 / 4) * std::min<i64>(r->E, r->nnz); }
 static i64 tile_count(const gm_route* r, i64 n_m, int n) { return ((r->nnz + n - 1) / n + std::min<i64>(r->E, r->nnz)) * ((n_m + kTileM - 1) / kTileM); }
 
 // Whether clusters of kRouteBlocks fit the current device (more than 8 blocks are not promised), found out once.
@@ -390,23 +390,19 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
   a.y = Y.data;
   a.y_stride = Y.row_stride;
   const bool vec = rows_aligned(P) && rows_aligned(Y);
-  // eight loads in flight per thread: of as many entries as rows have on average, and the rest of other columns
-  const i64 mean = (r->nnz + r->n_rows - 1) / r->n_rows;
-  const int columns = vec ? (mean > 4 ? 1 : mean > 2 ? 2 : mean > 1 ? 4 : 8) : (mean > 2 ? 4 : 8);
-  const i64 per = kSumThreads * columns * (vec ? 16 / static_cast<i64>(elem_size(P.dtype)) : 1), chunks = (a.width + per - 1) / per;
-  GM_TRY(sum_grid(chunks * r->n_rows, "sum"));
-  const auto go = [&](auto kernel) {
-    return launch(kernel, chunks * r->n_rows, kSumThreads, 0, st, 0, a, static_cast<int>(chunks));
-  };
+  // as many threads as a row has use for
   const auto typed2 = [&](auto* ti, auto* to) {
     using TI = std::remove_pointer_t<decltype(ti)>;
     using TO = std::remove_pointer_t<decltype(to)>;
-    const auto aligned = [&]<bool kVec>() {
-      if constexpr (kVec) {
-        if (columns == 1) return go(k_route_sum<TI, TO, true, 1>);
-        if (columns == 2) return go(k_route_sum<TI, TO, true, 2>);
-      }
-      return columns == 4 ? go(k_route_sum<TI, TO, kVec, 4>) : go(k_route_sum<TI, TO, kVec, 8>);
+    const auto aligned = [&]<bool kVec>() -> int {
+      constexpr int kUnits = kSumUnits<TI, kVec>;
+      const auto go = [&]<int kThreads>() -> int {
+        const i64 columns = kThreads * kUnits * (kVec ? 16 / sizeof(TI) : 1), chunks = (a.width + columns - 1) / columns;
+        GM_TRY(sum_grid(chunks * r->n_rows, "sum"));
+        return launch(k_route_sum<TI, TO, kVec, kUnits, kThreads>, chunks * r->n_rows, kThreads, 0, st, 0, a, static_cast<int>(chunks));
+      };
+      const int per = 32 * kUnits * (kVec ? 16 / static_cast<int>(sizeof(TI)) : 1);
+      return a.width <= per ? go.template operator()<32>() : a.width <= 2 * per ? go.template operator()<64>() : go.template operator()<128>();
     };
     return vec ? aligned.template operator()<true>() : aligned.template operator()<false>();
   };
