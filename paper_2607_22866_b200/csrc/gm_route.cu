@@ -8,10 +8,10 @@
 #include <new>
 
 #include "gm_host.h"
-#include "gm_r1_route.cuh"
-#include "gm_r2_product.cuh"
-#include "gm_r3_sum.cuh"
-#include "gm_r4_quantize.cuh"
+#include "gm_route_plan.cuh"
+#include "gm_route_product.cuh"
+#include "gm_route_sum.cuh"
+#include "gm_route_quantize.cuh"
 
 using gm::i64;
 

@@ -8,7 +8,7 @@
 #pragma once
 #include <cuda_fp8.h>
 
-#include "gm_r3_sum.cuh"
+#include "gm_route_sum.cuh"
 
 namespace gm {
 

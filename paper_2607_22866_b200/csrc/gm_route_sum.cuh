@@ -6,7 +6,7 @@
 // Both are bound by memory: P is read once (and dP written once), a row of Y or dY serves all entries of its row of R.  Sums are kept
 // in 32 bits, in the order of the row's entries, and rounded once.
 #pragma once
-#include "gm_r2_product.cuh"
+#include "gm_route_product.cuh"
 
 namespace gm {
 
