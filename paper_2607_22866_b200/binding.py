@@ -381,11 +381,14 @@ def _on_cuda(where: str, device: torch.device):
 def _there(call, device: torch.device, stream, *args, **kwargs):
     """The same call with the tensors' device and the given stream made current, so that what it allocates belongs to that stream; the
     inputs' memory is not given to others before the stream is done with it."""
+    if stream is not None and stream.device != device:
+        raise GmError(-1, call.__name__, f"a stream of {stream.device}, the tensors on {device}")
     with torch.cuda.device(device), torch.cuda.stream(stream):
         if stream is not None:
-            for t in args:
-                if isinstance(t, torch.Tensor) and t.is_cuda:
-                    t.record_stream(stream)
+            for a in args:
+                for t in (a.row_ptr, a.col, a.val) if isinstance(a, DeviceCSR) else (a,):
+                    if isinstance(t, torch.Tensor) and t.is_cuda:
+                        t.record_stream(stream)
         return call(*args, **kwargs)
 
 
@@ -452,9 +455,6 @@ def route_plan(R: DeviceCSR, stream=None) -> Route:
     device = R.row_ptr.device
     _on_cuda(where, device)
     if stream is not None or device.index != _current_device():
-        for t in (R.row_ptr, R.col, R.val):
-            if stream is not None and t.is_cuda:
-                t.record_stream(stream)
         return _there(route_plan, device, stream, R)
     if R.col.device != device or R.val.device != device:
         raise GmError(-1, where, "R's arrays are on different devices")

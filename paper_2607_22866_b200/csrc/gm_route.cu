@@ -134,13 +134,14 @@ struct Scratch {
   }
 };
 
-// What a tensor map can be laid over: 16-byte aligned base and outer strides, none of them zero, the inner dimension contiguous.
+// What a tensor map can be laid over: 16-byte aligned base and outer strides, none of them zero, the inner dimension contiguous, its runs apart.
 static bool map_fits(const gm_dense& M, bool rows_inner) {
   const i64 es = static_cast<i64>(elem_size(M.dtype));
   const i64 inner = rows_inner ? M.row_stride : M.col_stride, outer = rows_inner ? M.col_stride : M.row_stride;
   const i64 n_inner = rows_inner ? M.n_rows : M.n_cols, n_outer = rows_inner ? M.n_cols : M.n_rows;
   const auto ok = [&](i64 stride, i64 n) { return n <= 1 || (stride > 0 && stride * es % 16 == 0 && stride * es < (i64{1} << 40)); };
-  return reinterpret_cast<uintptr_t>(M.data) % 16 == 0 && (inner == 1 || n_inner <= 1) && ok(outer, n_outer) && ok(M.block_stride, M.n_blocks);
+  return reinterpret_cast<uintptr_t>(M.data) % 16 == 0 && (inner == 1 || n_inner <= 1) && ok(outer, n_outer) && (n_outer <= 1 || outer >= n_inner) &&
+         ok(M.block_stride, M.n_blocks);
 }
 
 static int pack(const gm_dense& M, Scratch* mem, int num_sms, gm_dense* out) {
@@ -503,7 +504,10 @@ int gm_route_status(const gm_route* route) { return guarded([&]() -> int { retur
 
 void gm_route_destroy(gm_route* route) {
   if (!route) return;
-  give_error_word(route->err);
+  guarded([&]() -> int {
+    give_error_word(route->err);
+    return GM_OK;
+  });
   delete route;
 }
 

@@ -238,6 +238,31 @@ def test_strides():
     assert torch.equal(gm.route_product(route, X[:1].expand(90, -1), W), gm.route_product(route, X[:1].repeat(90, 1), W))
 
 
+def test_unusual_layouts():
+    R = make_route(90, 4, 3, 5, drop=0.1)
+    route = gm.route_plan(R)
+    X, dP = randn((90, 136), BF16, 1), randn((R.nnz, 152), BF16, 3)
+    W = randn((152, 4, 136), BF16, 2).transpose(0, 1)  # blocks between each other's rows
+    V = W.contiguous()
+    assert torch.equal(gm.route_product(route, X, W), gm.route_product(route, X, V))
+    assert torch.equal(gm.route_product_dx(route, dP, W), gm.route_product_dx(route, dP, V))
+    W = randn((136, 152, 4), BF16, 2).permute(2, 1, 0)  # blocks innermost
+    V = W.contiguous()
+    assert torch.equal(gm.route_product(route, X, W), gm.route_product(route, X, V))
+    assert torch.equal(gm.route_product_dx(route, dP, W), gm.route_product_dx(route, dP, V))
+    long = randn((90 * 8 + 136,), BF16, 4)  # rows that share most of their values
+    X = long.as_strided((90, 136), (8, 1))
+    P = gm.route_product(route, X, V)
+    assert torch.equal(P, gm.route_product(route, X.contiguous(), V))
+    G = long.as_strided((R.nnz, 136), (8, 1)) if R.nnz <= 90 else torch.cat([long, long]).as_strided((R.nnz, 136), (8, 1))
+    assert torch.equal(gm.route_product(route, G, V, True), gm.route_product(route, G.contiguous(), V, True))
+    assert torch.equal(gm.route_product_dw(route, G, X), gm.route_product_dw(route, G.contiguous(), X.contiguous()))
+    assert torch.equal(gm.route_product_dw(route, G, G, True), gm.route_product_dw(route, G.contiguous(), G.contiguous(), True))
+    for rows in (1, 128):
+        for a, b in zip(gm.block_quantize(X, rows), gm.block_quantize(X.contiguous(), rows)):
+            assert torch.equal(a.float(), b.float())
+
+
 SUMS = [(1, 1, 1, 1), (1, 9, 5, 4096), (3, 40, 4, 130), (700, 5, 3, 1032), (64, 8, 9, 77), (300, 16, 6, 24), (5, 3, 2, 0), (20, 600, 300, 16), (0, 3, 2, 8)]
 
 
