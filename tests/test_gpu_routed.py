@@ -7,6 +7,7 @@ most n * 2^-23 * sum |terms| altogether.  f16 results below its smallest normal 
 import os
 import subprocess
 import sys
+import threading
 
 import numpy as np
 import pytest
@@ -536,6 +537,45 @@ def test_given_stream_and_route_of_another():
     del route, P
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(Y, want)
+
+
+def test_host_threads():
+    inputs = [layer_inputs(s) for s in (3, 40, 77)]
+    want = [[t.clone() for t in layer(*i)] for i in inputs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    got = layer(*inputs[k])
+                torch.cuda.current_stream().synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want[k])):
+                    wrong.append(k)
+        except Exception as e:  # pragma: no cover
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+def test_dx_with_the_librarys_own_scratch():
+    R = make_route(80, 5, 3, 6, drop=0.1)
+    route = gm.route_plan(R)
+    for K in (64, 77):
+        dP, W = randn((R.nnz, 40), BF16, 1), randn((5, 40, K), BF16, 2)
+        want, dX = gm.route_product_dx(route, dP, W), torch.full((80, K), 7.0, dtype=BF16, device="cuda")
+        b = gm.binding
+        d = dX.device
+        call = lambda terms: b.load_library().gm_route_product_dx(  # noqa: E731
+            route._h, b._dense(dP, "", d), b._dense(W, "", d), 0, b._dense(dX, "", d), terms, torch.cuda.current_stream().cuda_stream)
+        assert call(None) == 0 and torch.equal(dX, want)
+        assert call(dX.data_ptr() + 2) == -1  # not aligned
 
 
 def test_values_may_change_between_calls():
