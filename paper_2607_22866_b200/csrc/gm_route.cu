@@ -243,6 +243,8 @@ static size_t product_smem(int E, bool bits8) {
 }
 static_assert(std::max(kT5Smem<kTileN> + kScaleSmem<kTileN>, kT5Smem<kFewN> + kScaleSmem<kFewN>) + (kRouteMaxCols + 1) * 8 <= kMostSmem, "fits a block's shared memory");
 
+static_assert(kRouteMaxCols == GM_ROUTE_MAX_COLS, "as the header says");
+
 // Whether tiles of few places are the better ones: while a column has at most three quarters of such a tile's on average (64 columns of 1536 x 4096: with 8
 // places each 158 us against 165 with tiles of 256, in 8 bits 98 against 125; with 48 164 : 169 and 106 : 133, with 64 180 : 171 and 135 : 133).
 static bool few_places(const gm_route* r) { return r->nnz <= static_cast<i64>(kFewN * 3 / 4) * std::min<i64>(r->E, r->nnz); }
