@@ -685,7 +685,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
 
 // The same for columns of R with few places: they are the columns again (the instruction's N, 32 or 64), eight buffers of sums and ten stages
 // keep W on its way, and a thread has one row of W and up to 32 places, whose scales it reads from shared memory.  512 places in 128 columns of
-// 1536 x 4096: 154 us (5.2 TB/s of weights), 203 with tiles of 256 places.
+// 1536 x 4096: 154 us (5.2 TB/s of weights); in 64 columns 98, 125 with tiles of 256 places.
 // Warps: 0 copies by tensor map, 1 matrix instructions, 2 hands over what 12-15 copy by index, 3 scales, 4-11 results.
 constexpr int kFewSlot = kFewN + 128;
 template <bool kGather, bool kRowScales, typename TO>
