@@ -658,6 +658,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
           t5_fence_before();
           if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
         }
+        __syncwarp();  // every lane has read its scales: lane 0's arrival speaks for all of them
         if (lane == 0) mbar_arrive(&sb->empty[s]);
       }
       if (ok && some) {
@@ -791,6 +792,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
             for (int j = 0; j < 16; ++j) acc[c][j] = fmaf(__uint_as_float(v[j]), slot[half * each + c * 16 + j] * w, acc[c][j]);
           }
         t5_fence_before();
+        __syncwarp();  // every lane has read its scales: lane 0's arrivals speak for all of them
         if (lane == 0) {
           mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
           mbar_arrive(&sb->empty[s]);
