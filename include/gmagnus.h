@@ -345,6 +345,8 @@ int gm_route_plan(const gm_csr* R, int64_t* offsets, int32_t* rows, int32_t* ord
 /* GM_ERR_TIMEOUT when a kernel of an earlier call on this route gave up a wait (its results are then not valid), as
  * every further call on it does; GM_OK otherwise.  Does not wait: synchronise first to know about all of them. */
 int gm_route_status(const gm_route* route);
+/* Host only; may be called while work on the route is still under way, or before a graph that holds such calls is replayed: kernels need the borrowed
+ * arrays, not the route.  What gives up a wait after that is reported to nobody (never to another route): keep the route for its status. */
 void gm_route_destroy(gm_route* route);
 
 /* P (nnz x N, by place) = row of X times W[column]^T.  W: E blocks of N x K, of X's type (bf16 or f16); P: f32, bf16 or

@@ -180,6 +180,16 @@ struct SideStream {
   ~SideStream() { if (st) give_stream(st); }
 };
 
+void* page_locked(size_t bytes) {
+  OutsideCapture now;
+  void* p = nullptr;
+  if (cudaHostAlloc(&p, bytes, cudaHostAllocPortable | cudaHostAllocMapped) != cudaSuccess) {
+    cudaGetLastError();
+    return nullptr;
+  }
+  return p;
+}
+
 // Page-locked host memory that kernels write to and the host reads after a synchronisation: a plan takes one slot and
 // gives it back when it is destroyed.  (Copies to ordinary host variables took 12 to 25 us of host time each.)
 struct HostSlot {
@@ -199,12 +209,8 @@ static HostSlot* take_slot() {
   std::lock_guard<std::mutex> lock(g_slot_mutex);
   if (g_free_slots.empty()) {
     constexpr int kSlab = 64;
-    OutsideCapture now;
-    void* slab = nullptr;
-    if (cudaHostAlloc(&slab, kSlab * kHostSlotBytes, cudaHostAllocPortable | cudaHostAllocMapped) != cudaSuccess) {
-      cudaGetLastError();
-      return nullptr;
-    }
+    void* slab = page_locked(kSlab * kHostSlotBytes);
+    if (!slab) return nullptr;
     for (int i = kSlab - 1; i >= 0; --i)
       g_free_slots.push_back(reinterpret_cast<HostSlot*>(static_cast<char*>(slab) + i * kHostSlotBytes));
   }
@@ -218,13 +224,6 @@ static void give_slot(HostSlot* s) {
   std::lock_guard<std::mutex> lock(g_slot_mutex);
   g_free_slots.push_back(s);
 }
-
-int* take_error_word() {
-  HostSlot* s = take_slot();
-  return s ? s->err : nullptr;
-}
-void give_error_word(int* w) { give_slot(reinterpret_cast<HostSlot*>(w)); }  // (err is a slot's first member)
-static_assert(offsetof(HostSlot, err) == 0, "an error word is its slot");
 
 // ------------------------------------------------------------------------------------------------
 // plan

@@ -14,9 +14,7 @@ void* dev_alloc(size_t bytes, cudaStream_t st);           // the allocator hook,
 void dev_free(void* p, cudaStream_t st);
 int device_facts_basic(int* num_sms, int* smem_optin);    // of the current device, looked up once
 
-// Page-locked memory that a kernel writes its first problem to (DevError) and the host reads without a wait.
-int* take_error_word();
-void give_error_word(int* w);
+void* page_locked(size_t bytes);                          // host memory that kernels of every device may write to, or nullptr; kept for good
 
 #define GM_CUDA(expr)                                                                              \
   do {                                                                                             \

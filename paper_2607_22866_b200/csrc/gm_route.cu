@@ -24,7 +24,7 @@ struct gm_route {
   int32_t* rows = nullptr;
   int32_t* order = nullptr;
   int32_t* pos = nullptr;
-  int* err = nullptr;     // page-locked: the first problem of a kernel
+  gm::RouteWord word;     // whether a kernel gave up a wait
 };
 
 namespace gm {
@@ -211,9 +211,15 @@ static int map_out(CUtensorMap* map, const gm_dense& M) {
   return make_map(map, M.dtype, 3, M.data, dims, strides, box);
 }
 
+// (not destroyed at the process's end, where routes may still be given back)
+static RouteWords& words() {
+  static RouteWords* all = new RouteWords;
+  return *all;
+}
+
 static int route_ready(const gm_route* r) {
   if (!r) return fail(GM_ERR_INVALID_ARG, "route is null");
-  if (*static_cast<volatile int*>(r->err) != 0)
+  if (route_word_reported(r->word))
     return fail(GM_ERR_TIMEOUT, "an earlier call on this route gave up waiting on the device: its results are not valid");
   return GM_OK;
 }
@@ -348,7 +354,7 @@ static int product(const gm_route* r, const gm_dense& X, bool by_entry, const gm
   a.out = out.data;
   a.out_stride = out.row_stride;
   a.type = X.dtype == GM_BF16 ? 1 : 0;
-  a.err = r->err;
+  a.word = r->word;
   const auto typed = [&](auto* tag) {
     using TO = std::remove_pointer_t<decltype(tag)>;
     const auto sized = [&]<int kN>() {
@@ -468,8 +474,8 @@ int gm_route_plan(const gm_csr* R, int64_t* offsets, int32_t* rows, int32_t* ord
     r->E = static_cast<int>(R->n_cols);
     r->row_ptr = R->row_ptr;
     r->val = static_cast<const float*>(R->vals);
-    r->err = take_error_word();
-    if (!r->err) return drop(fail(GM_ERR_OOM, "no page-locked memory"));
+    r->word = words().take(page_locked);
+    if (!r->word.at) return drop(fail(GM_ERR_OOM, "no page-locked memory"));
     r->offsets = offsets;
     r->rows = rows;
     r->order = order;
@@ -507,7 +513,7 @@ int gm_route_status(const gm_route* route) { return guarded([&]() -> int { retur
 void gm_route_destroy(gm_route* route) {
   if (!route) return;
   guarded([&]() -> int {
-    give_error_word(route->err);
+    words().give(route->word);
     return GM_OK;
   });
   delete route;
@@ -597,7 +603,7 @@ int gm_route_product_dw(const gm_route* route, const gm_dense* dP, const gm_dens
     a.out_stride = dW->row_stride;
     a.out_align = out_align(*dW);
     a.type = dP->dtype == GM_BF16 ? 1 : 0;
-    a.err = route->err;
+    a.word = route->word;
     const i64 tiles = static_cast<i64>(a.E) * ((a.n_m + kTileM - 1) / kTileM) * ((a.n_j + kTileN - 1) / kTileN);
     CUtensorMap out_map = map_p;  // (used where the rows of dW are aligned)
     if (a.out_align >= 16) GM_TRY(map_out(&out_map, *dW));
@@ -773,7 +779,7 @@ int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_
     a.ws = static_cast<const float*>(ws.data);
     a.ws_block = ws.block_stride;
     a.ws_row = ws.row_stride;
-    a.err = route->err;
+    a.word = route->word;
     const bool few = few_places(route);
     const i64 tiles = tile_count(route, a.n_m, few ? kFewN : kTileN);
     const size_t smem = few ? product_smem<kFewN>(route->E, true) : product_smem<kTileN>(route->E, true);

@@ -20,6 +20,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "gm_route_words.h"
 #include "gm_t5.cuh"
 
 namespace gm {
@@ -59,7 +60,7 @@ struct ProductArgs {
   i64 xs_stride;
   const float* ws;      // ... and of W (E x groups of rows x blocks of k)
   i64 ws_block, ws_row;
-  int* err;
+  RouteWord word;
 };
 
 struct DwArgs {
@@ -74,7 +75,7 @@ struct DwArgs {
   i64 out_block, out_stride;
   int out_align;        // bytes that every 32nd value's address is a multiple of
   u32 type;
-  int* err;
+  RouteWord word;
 };
 
 template <typename T> __device__ __forceinline__ T from_float(float v);
@@ -265,7 +266,7 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
     }
   }
   copy_wait_all();
-  if (!ok && (thread & 31) == 0) dev_set_error(a.err, kDevTimeout);
+  if (!ok && (thread & 31) == 0) route_word_report(a.word);
 }
 
 template <int kN>
@@ -273,7 +274,7 @@ __device__ __forceinline__ void hand_over_rows(const ProductArgs& a, T5Block* b,
   const i64 pairs = gridDim.x >> 1, mine = (static_cast<i64>(n_tiles) - (blockIdx.x >> 1) + pairs - 1) / pairs * n_kb;
   bool ok = true;
   for (i64 it = 0; ok && it < mine; ++it) ok = hand_over<Shape<kN>::kStages>(b, static_cast<u32>(it));
-  if (!ok) dev_set_error(a.err, kDevTimeout);
+  if (!ok) route_word_report(a.word);
 }
 
 // Tiles of W (and of X with a row per place) by tensor map.  One warp; lane 0 has W, lane i 32 rows of X.
@@ -309,7 +310,7 @@ __device__ __forceinline__ void copy_tiles(const ProductArgs& a, const CUtensorM
     }
   }
   if (!ok) {
-    if (lane == 0) dev_set_error(a.err, kDevTimeout);
+    if (lane == 0) route_word_report(a.word);
     if (rank == 0) t5_drain_copies<kStages>(b, it);
   }
 }
@@ -470,7 +471,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
         if (ok) t5_commit(&b->sums_full[buf]);
       }
       if (!ok) {
-        dev_set_error(a.err, kDevTimeout);
+        route_word_report(a.word);
         t5_drain_matrix(b);
       }
     }
@@ -495,7 +496,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
       t5_fence_before();
       if (lane == 0) mbar_arrive_at(leader_bar(&b->sums_empty[buf]));
     }
-    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+    if (!ok && lane == 0) route_word_report(a.word);
   } else if (warp < 10) {
     gather_rows<kN, 2, false>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 192);
   } else {
@@ -579,7 +580,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
         }
       }
       if (!ok) {
-        dev_set_error(a.err, kDevTimeout);
+        route_word_report(a.word);
         t5_drain_matrix(b);
       }
     } else if (kGather && warp == 2 && lane == 0) {
@@ -606,7 +607,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
         }
       }
       copy_wait_all();
-      if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+      if (!ok && lane == 0) route_word_report(a.word);
     }
     __syncwarp();
   } else if (warp < 12) {
@@ -676,7 +677,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(512, 1)
         }
       }
     }
-    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+    if (!ok && lane == 0) route_word_report(a.word);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(48));
     if (kGather) gather_rows<kTileN, 1, true>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 384);
@@ -734,7 +735,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
         }
       }
       if (!ok) {
-        dev_set_error(a.err, kDevTimeout);
+        route_word_report(a.word);
         t5_drain_matrix(b);
       }
     }
@@ -764,7 +765,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
       }
     }
     copy_wait_all();
-    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+    if (!ok && lane == 0) route_word_report(a.word);
   } else if (warp < 12) {
     const int quad = warp & 3, half = (warp - 4) >> 2;
     u32 it = 0;
@@ -809,7 +810,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 512 : 384,
         }
       }
     }
-    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+    if (!ok && lane == 0) route_word_report(a.word);
   } else {
     gather_rows<kFewN, 1, false>(a, b, stage0, b->index, off, part, n_tiles, n_mt, threadIdx.x - 384);
   }
@@ -901,7 +902,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
         }
       }
       if (!ok) {
-        dev_set_error(a.err, kDevTimeout);
+        route_word_report(a.word);
         if (rank == 0) t5_drain_copies<kStages>(b, it);
       }
     }
@@ -930,7 +931,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
         ++n_done;
       }
       if (!ok) {
-        dev_set_error(a.err, kDevTimeout);
+        route_word_report(a.word);
         t5_drain_matrix(b);
       }
     }
@@ -941,7 +942,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
       bool ok = true;
       for (DwWalk t(a, off); ok && t.more(); t.next())
         for (int p = t.p0; ok && p < t.p1; p += 64, ++it) ok = hand_over<kStages>(b, it);
-      if (!ok) dev_set_error(a.err, kDevTimeout);
+      if (!ok) route_word_report(a.word);
     }
     __syncwarp();
   } else if (warp >= 6) {
@@ -989,7 +990,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
       }
     }
     copy_wait_all();
-    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+    if (!ok && lane == 0) route_word_report(a.word);
   } else if (warp >= 2) {
     const int quad = warp & 3;
     u32 n_done = 0, run = 0;
@@ -1046,7 +1047,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
       }
     }
     if (lane == 0) tma_store_done();
-    if (!ok && lane == 0) dev_set_error(a.err, kDevTimeout);
+    if (!ok && lane == 0) route_word_report(a.word);
   }
   __syncwarp();
   t5_end(tmem);
