@@ -484,7 +484,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 352 : 192,
       const Part t = part_at(off, part, a.E, static_cast<int>(id / static_cast<u32>(n_mt)));
       const int m = static_cast<int>(id % static_cast<u32>(n_mt)) * kTileM + rank * 128 + quad * 32 + lane;
       const u32 buf = n_done % kBuffers;
-      ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done / kBuffers) & 1));
+      ok = __all_sync(0xffffffffu, t5_wait_sum(&b->sums_full[buf], (n_done / kBuffers) & 1, n_kb));
       if (!ok) break;
       t5_fence_after();
       for (int c = 0; c < t.n; c += 16) {
@@ -1000,7 +1000,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(480, 1)
       TO* out = static_cast<TO*>(a.out) + static_cast<i64>(e) * a.out_block + static_cast<i64>(m - lane) * a.out_stride + t.j0;
       const u32 buf = n_done & 1;
       if (t.p0 < t.p1) {
-        ok = __all_sync(0xffffffffu, t5_wait(&b->sums_full[buf], (n_done >> 1) & 1));
+        ok = __all_sync(0xffffffffu, t5_wait_sum(&b->sums_full[buf], (n_done >> 1) & 1, (t.p1 - t.p0 + 63) / 64));
         if (!ok) break;
         t5_fence_after();
         const u32 sums = tmem + buf * kTileN + (static_cast<u32>(quad * 32) << 16);

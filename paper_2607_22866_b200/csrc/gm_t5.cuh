@@ -12,14 +12,23 @@ namespace gm {
 __device__ __forceinline__ void grid_launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Polls of a barrier before a wait gives up: a failed try_wait has itself waited for a while, so this is far above any
-// wait that ends (the longest is for one tile's products, under 2 ms).
+// Polls of a barrier before a wait gives up: a failed try_wait has itself waited for 1.5 us, so this is six seconds, far above any wait for a
+// stage, its copies or a buffer of sums (microseconds).
 constexpr int kT5SpinLimit = 1 << 22;
 
 // Without back-off: these barriers hand over within a microsecond.
 __device__ __forceinline__ bool t5_wait(u64* bar, u32 parity) {
   for (int i = 0; i < kT5SpinLimit; ++i)
     if (mbar_try_wait(bar, parity)) return true;
+  return false;
+}
+// For the end of a sum, which lasts as long as its stages (0.2 to 0.5 us each: a sum over 2^30 values or places takes seconds), the limit grows
+// with them: another one for each kT5StagesPerLimit.
+constexpr u32 kT5StagesPerLimit = 1 << 20;
+static_assert(kT5SpinLimit >= 2 * kT5StagesPerLimit, "twice the time of that many stages if they took a microsecond each, and a poll no more");
+__device__ __forceinline__ bool t5_wait_sum(u64* bar, u32 parity, u32 stages) {
+  for (u32 i = 0; i <= stages / kT5StagesPerLimit; ++i)
+    if (t5_wait(bar, parity)) return true;
   return false;
 }
 // ---- pairs of blocks (clusters of two): the even one leads, its thread issues the matrix instructions for both

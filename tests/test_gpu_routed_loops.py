@@ -52,3 +52,24 @@ def test_scaled_few_places_over_many_tiles(n, E, k, N, K, by_entry, rows):
         assert torch.equal(P, gm.route_product_scaled(route, Xq, Xs, Wq, Ws, by_entry, dtype=F32))
     torch.cuda.synchronize()
     route.status()
+
+
+@pytest.mark.parametrize("by_entry", [False, True])
+def test_dw_of_a_column_of_many_places(by_entry):
+    # half a million stages in one sum; of -1, 0 and 1, whose partial sums stay far below 2^24: exact in any order
+    n, entries = 5000, 32_000_000 + 37
+    row_ptr = (torch.arange(n + 1, device="cuda") * entries) // n
+    R = gm.DeviceCSR(n, 2, row_ptr, torch.ones(entries, dtype=torch.int32, device="cuda"), torch.ones(entries, device="cuda"))
+    route = gm.route_plan(R)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ones = lambda rows: torch.randint(-1, 2, (rows, 8), generator=g, device="cuda", dtype=torch.int8).bfloat16()  # noqa: E731
+    dP, X = ones(entries), ones(entries if by_entry else n)
+    dW = gm.route_product_dw(route, dP, X, by_entry, dtype=F32)
+    ref = torch.zeros(8, 8, dtype=torch.float64, device="cuda")
+    for a in range(0, entries, 1 << 22):
+        d = dP[a: a + (1 << 22)].double()
+        ref += d.T @ (X[a: a + (1 << 22)] if by_entry else X[route.rows[a: a + (1 << 22)].long()]).double()
+    assert float(ref.abs().max()) < 2.0 ** 20
+    assert torch.equal(dW[1].double(), ref) and not dW[0].any()
+    torch.cuda.synchronize()
+    route.status()
