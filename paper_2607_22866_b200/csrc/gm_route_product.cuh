@@ -213,7 +213,8 @@ __device__ __forceinline__ void gather_rows(const ProductArgs& a, T5Block* b, u3
                                             int n_mt, int thread) {
   using S = Shape<kN>;
   CopyQueue<S::kStages> queue(b);
-  const int n_kb = (a.n_k * kValueBytes + kRowBytes - 1) / kRowBytes, c = thread & 7, r0 = thread >> 3, lane = thread & 31;
+  constexpr int kStep = kRowBytes / kValueBytes;
+  const int n_kb = (a.n_k + kStep - 1) / kStep, c = thread & 7, r0 = thread >> 3, lane = thread & 31;
   const u32 at = kHalf + r0 * kRowBytes + ((c ^ (r0 & 7)) << 4);  // (rows r0 + 16 i: the same swizzle)
   constexpr int kApart = 16, kRows = kN / 2 / kApart;  // a thread's rows: r0 + 16 i
   const int my_row = (thread >> 5) * 4 + (lane & 3) + kApart * (lane >> 2);  // the one whose index this lane brings in for its warp

@@ -73,3 +73,25 @@ def test_dw_of_a_column_of_many_places(by_entry):
     assert torch.equal(dW[1].double(), ref) and not dW[0].any()
     torch.cuda.synchronize()
     route.status()
+
+
+@pytest.mark.parametrize("kind", ["16 bits", "8 bits"])
+def test_sums_over_more_than_2_to_30_values(kind):
+    # rows whose bytes pass 2^31, in sums that last for seconds; almost all values are zero, the others small whole numbers: exact
+    K = 2 ** 30 + 72
+    R = gm.DeviceCSR(1, 1, torch.tensor([0, 1], device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.ones(1, device="cuda"))
+    route = gm.route_plan(R)
+    X, W = (torch.zeros(K, dtype=BF16, device="cuda") for _ in range(2))
+    at = torch.tensor([0, 63, 64, 2 ** 20 + 5, 2 ** 29, 2 ** 30 - 1, 2 ** 30, 2 ** 30 + 63, 2 ** 30 + 64, K - 1], device="cuda")
+    X[at], W[at] = torch.arange(1, 11, device="cuda").bfloat16(), torch.arange(10, 0, -1, device="cuda").bfloat16()
+    want = float((X[at].double() * W[at].double()).sum())
+    if kind == "16 bits":
+        P = gm.route_product(route, X[None], W[None, None], dtype=F32)
+        dX = gm.route_product_dx(route, P.bfloat16(), W[None, None], dtype=F32)
+        assert torch.equal(dX, (float(P.bfloat16()) * W.float())[None])
+    else:
+        e4m3, scales = torch.float8_e4m3fn, torch.ones(1, -(-K // 128), device="cuda")
+        P = gm.route_product_scaled(route, X.to(e4m3)[None], scales, W.to(e4m3)[None, None], scales[None], dtype=F32)
+    assert float(P) == want
+    torch.cuda.synchronize()
+    route.status()
