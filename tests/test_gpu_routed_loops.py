@@ -10,7 +10,7 @@ import pytest
 import torch
 
 import paper_2607_22866_b200 as gm
-from test_gpu_routed import BF16, F16, F32, close, make_route, product_reference, randn
+from test_gpu_routed import BF16, F16, F32, close, dw_reference, dx_reference, make_route, product_reference, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -93,5 +93,92 @@ def test_sums_over_more_than_2_to_30_values(kind):
         e4m3, scales = torch.float8_e4m3fn, torch.ones(1, -(-K // 128), device="cuda")
         P = gm.route_product_scaled(route, X.to(e4m3)[None], scales, W.to(e4m3)[None, None], scales[None], dtype=F32)
     assert float(P) == want
+    torch.cuda.synchronize()
+    route.status()
+
+
+# n, E, k, N, K: tiles of 256 places (six stages a block of threads) and of 64 (ten): as many blocks of 64 values as stages, one more, many
+LOOPS = [(3000, 9, 4, 1000, 840), (3000, 9, 4, 1032, 384), (3000, 9, 4, 1032, 448), (700, 64, 4, 520, 1496), (700, 64, 4, 520, 640), (700, 64, 4, 520, 704)]
+
+
+def few(R):
+    return R.nnz <= 48 * R.n_cols
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("by_entry", [False, True])
+@pytest.mark.parametrize("n,E,k,N,K", LOOPS)
+def test_products_over_many_tiles(n, E, k, N, K, by_entry, dtype):
+    R = make_route(n, E, k, 29 * n + K, drop=0.05, skew=0.7)
+    route = gm.route_plan(R)
+    assert few(R) == (E == 64) and tiles(R, 64 if few(R) else 256, N) > 74 * 1.25
+    X, W, dP = randn((R.nnz if by_entry else n, K), dtype, 1), randn((E, N, K), dtype, 2), randn((R.nnz, N), dtype, 3)
+    P = gm.route_product(route, X, W, by_entry, dtype=F32)
+    ref, mag = product_reference(R, X, W, by_entry)
+    close(P, ref, mag, K)
+    close_norm(P, ref, K)
+    dX = gm.route_product_dx(route, dP, W, by_entry, dtype=F32)
+    ref, mag = dx_reference(R, dP, W, by_entry)
+    close(dX, ref, mag, N + k)
+    close_norm(dX, ref, N + k)
+    dW = gm.route_product_dw(route, dP, X, by_entry, dtype=F32)
+    ref, mag, most = dw_reference(R, dP, X, by_entry)
+    close(dW, ref, mag, most)
+    close_norm(dW, ref, most)
+    half = [gm.route_product(route, X, W, by_entry), gm.route_product_dx(route, dP, W, by_entry), gm.route_product_dw(route, dP, X, by_entry)]
+    for a, b in zip((P, dX, dW), half):  # the same sums, rounded
+        assert b.dtype == dtype and torch.equal(a.to(dtype), b)
+    for _ in range(3):
+        assert torch.equal(P, gm.route_product(route, X, W, by_entry, dtype=F32)) and torch.equal(dW, gm.route_product_dw(route, dP, X, by_entry, dtype=F32))
+    torch.cuda.synchronize()
+    route.status()
+
+
+# tiles of 256 places, two of them per pair of blocks and more, with more blocks of 128 values than stages, buffers of sums and slots of scales
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("by_entry", [False, True])
+@pytest.mark.parametrize("n,E,k,N,K", [(3000, 9, 4, 1032, 1680), (2500, 8, 5, 1536, 1168)])
+def test_scaled_many_places_over_many_tiles(n, E, k, N, K, by_entry, rows):
+    R = make_route(n, E, k, 31 * n, drop=0.05, skew=0.7)
+    route = gm.route_plan(R)
+    assert not few(R) and tiles(R, 256, N) > 74 * 1.25
+    (Xq, Xs, Wq, Ws), x, w = scaled_inputs(R.nnz if by_entry else n, E, N, K, rows)
+    P = gm.route_product_scaled(route, Xq, Xs, Wq, Ws, by_entry, dtype=F32)
+    ref, mag = product_reference(R, x, w, by_entry)
+    close(P, ref, mag, K + 3)
+    close_norm(P, ref, K + 3)
+    for dtype in (BF16, F16):
+        assert torch.equal(P.to(dtype), gm.route_product_scaled(route, Xq, Xs, Wq, Ws, by_entry, dtype=dtype))
+    for _ in range(5):
+        assert torch.equal(P, gm.route_product_scaled(route, Xq, Xs, Wq, Ws, by_entry, dtype=F32))
+    torch.cuda.synchronize()
+    route.status()
+
+
+def test_large_tiles_with_the_most_columns():
+    # 2048 columns with more than 48 places each on average: the shared memory of large tiles and of the most columns
+    n, E, N, K = 30000, 2048, 24, 72
+    R = make_route(n, E, 9, 21, drop=0.02)
+    assert not few(R)
+    route = gm.route_plan(R)
+    X, W = randn((n, K), BF16, 1), randn((E, N, K), BF16, 2)
+    P = gm.route_product(route, X, W, dtype=F32)
+    ref, mag = product_reference(R, X, W, False)
+    close(P, ref, mag, K)
+    close_norm(P, ref, K)
+    for rows in (1, 128):
+        (Xq, Xs, Wq, Ws), x, w = scaled_inputs(n, E, N, K, rows)
+        P = gm.route_product_scaled(route, Xq, Xs, Wq, Ws, dtype=F32)
+        ref, mag = product_reference(R, x, w, False)
+        close(P, ref, mag, K + 3)
+        close_norm(P, ref, K + 3)
+    dP = randn((R.nnz, N), BF16, 3)
+    dX, dW = gm.route_product_dx(route, dP, W, dtype=F32), gm.route_product_dw(route, dP, X, dtype=F32)
+    ref, mag = dx_reference(R, dP, W, False)
+    close(dX, ref, mag, N + 9)
+    close_norm(dX, ref, N + 9)
+    ref, mag, most = dw_reference(R, dP, X, False)
+    close(dW, ref, mag, most)
+    close_norm(dW, ref, most)
     torch.cuda.synchronize()
     route.status()
