@@ -388,10 +388,8 @@ static int sum_rows(const gm_route* r, const gm_dense& P, bool weighted, const g
   a.val = weighted ? r->val : nullptr;
   a.offsets = r->offsets;
   a.rows = r->rows;
-  a.order = r->order;
   a.pos = r->pos;
   a.E = r->E;
-  a.n_rows = r->n_rows;
   a.entries = r->nnz;
   a.width = static_cast<int>(Y.n_cols);
   a.p = P.data;
@@ -656,7 +654,6 @@ int gm_route_sum_grads(const gm_route* route, const gm_dense* dY, const gm_dense
     a.rows = route->rows;
     a.pos = route->pos;
     a.E = route->E;
-    a.n_rows = route->n_rows;
     a.entries = route->nnz;
     a.width = static_cast<int>(P->n_cols);
     a.p = V.data;

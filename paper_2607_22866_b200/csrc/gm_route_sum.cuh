@@ -12,10 +12,6 @@ namespace gm {
 
 template <typename T> struct Vec8;  // eight consecutive values as floats
 template <> struct Vec8<float> {
-  static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  }
   static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
@@ -102,10 +98,9 @@ struct SumArgs {
   const float* val;       // nullptr: every entry counts once
   const i64* offsets;
   const int32_t* rows;    // by place
-  const int32_t* order;   // by place
   const int32_t* pos;     // by entry
   int E;
-  i64 n_rows, entries;
+  i64 entries;
   int width;
   const void* p;
   i64 p_stride;

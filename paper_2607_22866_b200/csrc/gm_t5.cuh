@@ -66,10 +66,6 @@ __device__ __forceinline__ void tma_load_3d(u32 dst, const CUtensorMap* map, int
 
 // From this block's memory into a result, by tensor map: what lies outside is not written.  One thread; the memory may be written again after
 // tma_store_read(), and the block leave after tma_store_done().
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, u32 src) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n\tcp.async.bulk.commit_group;" ::"l"(map), "r"(x), "r"(y), "r"(src)
-               : "memory");
-}
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, u32 src) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];\n\tcp.async.bulk.commit_group;" ::"l"(map), "r"(x), "r"(y), "r"(z),
                "r"(src)
