@@ -397,13 +397,20 @@ class Route:
 
     offsets (n_cols + 1, int64): first place of every column, and behind the last one the number of routed entries;
     rows, order (nnz, int32): row and entry of R at every place; pos (nnz, int32): place of every entry.
-    Keeps R alive, whose row_ptr and val it borrows.  It may go before its work is done, or before a graph with its calls is replayed (which needs R's
+    Keeps R alive, whose row_ptr and val it borrows: values may change in place; calls that read an array of R that has been replaced are refused.  It may go before its work is done, or before a graph with its calls is replayed (which needs R's
     arrays); status() is then gone with it."""
 
     def __init__(self, handle, R: DeviceCSR, stream: int, memory: torch.Tensor):
         self._h, self.R, self._stream, self._memory = handle, R, stream, memory
         self.n_rows, self.n_cols, self.nnz, self.device = R.n_rows, R.n_cols, R.nnz, memory.device
         self._index = self.device.index
+        self._row_ptr, self._val = R.row_ptr, R.val  # what the library has the addresses of
+        self._at = R.row_ptr.data_ptr(), R.val.data_ptr()
+
+    def _reads(self, where: str, val: bool):
+        """R's arrays must be the ones that the route was made of, wherever a call reads them."""
+        if self.R.row_ptr.data_ptr() != self._at[0] or (val and self.R.val.data_ptr() != self._at[1]):
+            raise GmError(-1, where, "R has got other arrays since its route was made: change values in place, or make another route")
 
     def _places(self, k: int) -> torch.Tensor:
         first = 2 * (self.n_cols + 1) + k * self.nnz
@@ -433,7 +440,7 @@ class Route:
         stream = _current_raw_stream(self._index)
         if stream != self._stream:  # not the one its memory belongs to
             s = torch.cuda.current_stream(self.device)
-            for t in (self._memory, self.R.row_ptr, self.R.val):
+            for t in (self._memory, self._row_ptr, self._val):
                 t.record_stream(s)
         return stream
 
@@ -491,6 +498,8 @@ def route_product_dx(route: Route, dP: torch.Tensor, W: torch.Tensor, by_entry: 
         return _there(route_product_dx, device, stream, route, dP, W, by_entry, dtype)
     _dims(dP, where, "dP", 2)
     _dims(W, where, "W", 3)
+    if not by_entry:
+        route._reads(where, False)
     rows, K = route.nnz if by_entry else route.n_rows, W.shape[2]
     dX = _empty(dP, rows, K, dtype)
     terms = None if by_entry else torch.empty(route.nnz * (K + 7 & ~7), dtype=torch.float32, device=device)
@@ -518,6 +527,7 @@ def route_sum(route: Route, P: torch.Tensor, weighted: bool = True, dtype=None, 
     if stream is not None or route._index != _current_device():
         return _there(route_sum, device, stream, route, P, weighted, dtype)
     _dims(P, where, "P", 2)
+    route._reads(where, weighted)
     Y = _empty(P, route.n_rows, P.shape[1], dtype)
     _check(load_library().gm_route_sum(route._h, _dense(P, where, device), weighted, _result(Y, route.n_rows, P.shape[1]), route._current_stream()), where)
     return Y
@@ -530,6 +540,7 @@ def route_sum_grads(route: Route, dY: torch.Tensor, P: torch.Tensor, stream=None
         return _there(route_sum_grads, device, stream, route, dY, P)
     _dims(dY, where, "dY", 2)
     _dims(P, where, "P", 2)
+    route._reads(where, True)
     dP = _empty(P, route.nnz, P.shape[1], None)
     dval = torch.empty(route.nnz, dtype=torch.float32, device=device)
     _check(load_library().gm_route_sum_grads(route._h, _dense(dY, where, device), _dense(P, where, device), _result(dP, route.nnz, P.shape[1]),
