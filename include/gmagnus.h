@@ -309,13 +309,14 @@ int gm_row_products_noalloc(const gm_csr* A, const gm_csr* B, int64_t* ip_out_de
  * The entries are used in the order of their columns ("places" p): column e has the places [offsets[e],
  * offsets[e+1]), within a column the order of R is kept.  An entry whose column is outside [0, E) (-1, say) is
  * routed nowhere: it has a place behind all others, its row of a result is zero, and it adds nothing.
- * Unlike in the products above, columns need not ascend within a row.
+ * Unlike in the products above, columns need not ascend within a row.  row_ptr has to ascend from 0 to nnz (it is not checked: nothing is read out of
+ * range if it does not, but entries in front of its first or behind its last row do not take part in every call alike).
  *
  * None of these calls waits for the device.  Work is enqueued on `cuda_stream`; scratch memory comes from the
  * allocator hook and goes back to it, with that stream, before the call returns.  They can be captured into a
  * CUDA graph, with a hook that serves captures (or the default pool); what they borrow has to live as long as the graph.
- * Sums are kept in 32 bits, in an order that depends on the shapes and on R's structure only: the same call gives the
- * same bits.  No call here records anything for automatic differentiation: gradients have calls of their own.
+ * Sums are kept in 32 bits, in an order that depends on the shapes, on R's structure and, for dval of gm_route_sum_grads, on whether rows start on
+ * 16 bytes: the same call on arrays laid out the same gives the same bits.  No call here records anything for automatic differentiation: gradients have calls of their own.
  * ------------------------------------------------------------------------------------------- */
 
 /* A dense array in device memory: n_blocks matrices of n_rows x n_cols, element strides (not negative; 0 repeats).
@@ -370,7 +371,8 @@ int gm_route_sum_grads(const gm_route* route, const gm_dense* dY, const gm_dense
  * are not finite become NaN.  Q: X's shape, S: n_blocks x ceil(n_rows / block_rows) x ceil(n_cols / 128) f32, both contiguous. */
 int gm_block_quantize(const gm_dense* X, int block_rows, const gm_dense* Q, const gm_dense* S, void* cuda_stream);
 /* gm_route_product with e4m3 factors: P[p,n] = sum over blocks b of 128 k's of Xs[row,b] * Ws[col,n,b] * sum_k Xq * Wq.  Xs: a scale
- * for each row and block; Ws: for each 128 rows (ceil(N / 128)) or each row (N) of a block of W.  P: f32, bf16 or f16. */
+ * for each row and block; Ws: for each 128 rows (ceil(N / 128)) or each row (N) of a block of W.  P: f32, bf16 or f16.
+ * Xs * Ws is formed first, in 32 bits: where it leaves the normal range of a float, so does the block's part of the result. */
 int gm_route_product_scaled(const gm_route* route, const gm_dense* Xq, const gm_dense* Xs, int by_entry, const gm_dense* Wq, const gm_dense* Ws,
                           const gm_dense* P, void* cuda_stream);
 

@@ -252,7 +252,8 @@ static_assert(std::max(kT5Smem<kTileN> + kScaleSmem<kTileN>, kT5Smem<kFewN> + kS
 static_assert(kRouteMaxCols == GM_ROUTE_MAX_COLS, "as the header says");
 
 // Whether tiles of few places are the better ones: while a column has at most three quarters of such a tile's on average (64 columns of 1536 x 4096: with 8
-// places each 158 us against 165 with tiles of 256, in 8 bits 98 against 125; with 48 164 : 169 and 106 : 133, with 64 180 : 171 and 135 : 133).
+// places each 158 us against 165 with tiles of 256, in 8 bits 98 against 125; with 48 164 : 169 and 106 : 133, with 64 180 : 171 and 135 : 133).  Measured with
+// columns that are all alike: where few columns of very many hold most entries, the average is low and these, too, go in tiles of 64.
 static bool few_places(const gm_route* r) { return r->nnz <= static_cast<i64>(kFewN * 3 / 4) * std::min<i64>(r->E, r->nnz); }
 static i64 tile_count(const gm_route* r, i64 n_m, int n) { return ((r->nnz + n - 1) / n + std::min<i64>(r->E, r->nnz)) * ((n_m + kTileM - 1) / kTileM); }
 

@@ -10,7 +10,7 @@
 // What bounds the pairs is the way from L2 to the SMs: 32 KB a stage and block, at 85 GB/s per SM 380 ns, which is the library's matrix
 // product's pace (1.62 PFLOP/s), too; these reach 1.46 PFLOP/s with 256 places a tile (16384 places x 2048 x 4096, a row per place), 1.31 with
 // rows by index, 1.15 with the 205 places that a tile holds on average at 32768 places in 64 columns of skewed popularity.
-// The places are the instruction's N: a column's places are cut into equal parts, and a part of 33 places costs matrix time for 64.
+// The places are the instruction's N: a column's places are cut into as few parts as there can be, and a part of 33 places costs matrix time for 64.
 // The sums have two buffers, so that the results of one tile are taken out while the next one is summed up.  Every role of a block finds its
 // tiles by itself; that costs each of them a fraction of a microsecond a tile, and took up to 0.9 with divisions in 64 bits.
 //
@@ -73,7 +73,7 @@ struct DwArgs {
   i64 x_stride;
   void* out;
   i64 out_block, out_stride;
-  int out_align;        // bytes that every 32nd value's address is a multiple of
+  int out_align;        // bytes that the rows' addresses are multiples of
   u32 type;
   RouteWord word;
 };
@@ -106,7 +106,8 @@ struct T5Block {
   int index[2 * kIndexSlot];
 };
 
-// Places of each column, cut into parts of at most kN places that differ by less than 32 in size.
+// Places of each column, cut into as few parts of at most kN places as there can be: all of one size, a multiple of 32, but for the last one, which has
+// what is left (257 places are 160 and 97, and 1793 seven times 256 and one).
 struct Part { int e, first, n; };
 __device__ __forceinline__ int round32(int n) { return (n + 31) & ~31; }
 template <int kN> __device__ __forceinline__ int part_count(int places) { return (places + kN - 1) / kN; }
