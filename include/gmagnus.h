@@ -316,7 +316,8 @@ int gm_row_products_noalloc(const gm_csr* A, const gm_csr* B, int64_t* ip_out_de
  * allocator hook and goes back to it, with that stream, before the call returns.  They can be captured into a
  * CUDA graph, with a hook that serves captures (or the default pool); what they borrow has to live as long as the graph.
  * Sums are kept in 32 bits, in an order that depends on the shapes, on R's structure and, for dval of gm_route_sum_grads, on whether rows start on
- * 16 bytes: the same call on arrays laid out the same gives the same bits.  No call here records anything for automatic differentiation: gradients have calls of their own.
+ * 16 bytes: the same call on arrays laid out the same gives the same bits.  No call here records anything for automatic
+ * differentiation: gradients have calls of their own.
  * ------------------------------------------------------------------------------------------- */
 
 /* A dense array in device memory: n_blocks matrices of n_rows x n_cols, element strides (not negative; 0 repeats).

@@ -397,8 +397,9 @@ class Route:
 
     offsets (n_cols + 1, int64): first place of every column, and behind the last one the number of routed entries;
     rows, order (nnz, int32): row and entry of R at every place; pos (nnz, int32): place of every entry.
-    Keeps R alive, whose row_ptr and val it borrows: values may change in place; calls that read an array of R that has been replaced are refused.  It may go before its work is done, or before a graph with its calls is replayed (which needs R's
-    arrays); status() is then gone with it."""
+    Keeps R alive, whose row_ptr and val it borrows: values may change in place; calls that read an array of R that has been
+    replaced are refused.  It may go before its work is done, and status() goes with it.  A graph reads R's arrays at every replay, and
+    those of the route if the route was made before the capture: keep R, and such a route, as long as the graph."""
 
     def __init__(self, handle, R: DeviceCSR, stream: int, memory: torch.Tensor):
         self._h, self.R, self._stream, self._memory = handle, R, stream, memory
